@@ -425,6 +425,113 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
                            int32_t n_iter, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * Paged K/V cache.  Before a prompt is factorised (p1) its tokens run through the model in chunks,
+ * each chunk attending exactly to all positions up to its own; drafted tokens are verified in the
+ * same way, and so is a sequence decoded that is too short for a selection to pay.  K and V of such
+ * sequences lie in pages of a pool that several sequences share:
+ *
+ *   lrqk_pages_append   the new tokens' rows go into their pages, in 8 bits if the pages hold 8 bits
+ *   lrqk_chunk_attend   exact attention of the new tokens over the paged rows
+ *   lrqk_pages_read     rows of the pages as dense per-head arrays: what lrqk_prefill_factorize, the
+ *                       host store (K_host, V_host) and the lite rows are made from
+ *
+ * Sequence b has kv_len[b] positions, the last n = start[b+1] - start[b] of which are its new tokens
+ * (n >= 0; as long as start is ascending, each sequence may have another number).  Token i of them
+ * is row start[b] + i of the packed arrays and position kv_len[b] - n + i.  Position p is row
+ * p mod page of page table[b][p / page].
+ *   - A table entry outside [0, n_pages) is no page: rows written to it are dropped, rows read from it
+ *     are left alone in the output, positions on it take no part in an attention.  Several
+ *     sequences may share a page (a common prefix); a row that two calls, or two sequences of a
+ *     call, write holds what either wrote.
+ *   - Positions below 0 or from l_max on do not exist (the same rules).
+ *   - Rows of the packed arrays before start[0] and from start[B] on belong to no sequence: not read,
+ *     and left as they were in outputs.
+ *   - Rows of a page that no position reaches may hold anything, infinities and NaN included.
+ * start, kv_len and table are device memory and are read by the kernels only: a captured call follows
+ * what they hold when it is replayed.
+ *
+ * 8-bit pages: every 32 elements of a row share a scale 2^e, the smallest power of two with
+ * e >= -110 for which none of them exceeds the largest code (448 for e4m3, 127 for i8), kept as the
+ * byte e + 127.  Codes are x 2^-e rounded to the nearest, ties to even; since the scale is a power of
+ * two that is the only rounding, and a code times its scale is exact in bf16 and fp32.  32
+ * elements with an infinity or a NaN among them get the scale byte 255 and read as NaN.
+ */
+enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 = 3 };
+
+/*
+ *   T          rows of the packed arrays (q, out, k_new, v_new), 1 <= T < 2^24
+ *   n_max      new tokens of any one sequence, at most; chooses between kernels, results do not
+ *              depend on it
+ *   l_max      positions of any one sequence, at most, 1 <= l_max < 2^24
+ *   l_cap      rows allocated per head in the dense arrays of lrqk_pages_read; 0 means l_max
+ *   page       positions per page: a power of two, 1 <= page <= 1024
+ *   n_pages    pages of the pool
+ *   max_pages  entries of a sequence's row of the table, max_pages * page >= l_max
+ *   kv_dtype   LRQK_KV_*: type of q, out, k_new, v_new and the dense arrays
+ *   page_dtype LRQK_PAGE_*: type of the rows in the pool; BF16 and F32 need the same kv_dtype
+ *   d = 128, Hq a multiple of Hkv, Hq/Hkv <= 8, B * Hq <= 65535, T * Hq < 2^31, scale finite
+ */
+typedef struct lrqk_pages_shape {
+  int32_t B, Hq, Hkv, d, T, n_max, l_max, l_cap, page, n_pages, max_pages;
+  int32_t kv_dtype, page_dtype;
+  float scale;
+} lrqk_pages_shape;
+
+/* All device memory, 16-byte aligned. */
+typedef struct lrqk_pages {
+  void* K;              /* page_dtype [n_pages,Hkv,page,d] */
+  void* V;              /* page_dtype [n_pages,Hkv,page,d] */
+  uint8_t* K_scale;     /* 8-bit pages: [n_pages,Hkv,page,d/32]; else not looked at (may be NULL) */
+  uint8_t* V_scale;     /* likewise */
+  const int32_t* table;  /* [B,max_pages] */
+  const int32_t* start;  /* [B+1] */
+  const int32_t* kv_len; /* [B] */
+} lrqk_pages;
+
+/* Host-only check of a shape against the limits above. LRQK_OK / LRQK_EINVAL / LRQK_ESHAPE. */
+int lrqk_validate_pages(const lrqk_pages_shape* shape);
+
+/* Bytes of device workspace lrqk_chunk_attend needs for this shape (0 on a bad shape).  Contents
+ * need no initialisation; calls that overlap, and graphs whose replays overlap, need one each. */
+size_t lrqk_pages_workspace_bytes(const lrqk_pages_shape* shape);
+
+/*
+ * g1 — the new tokens' rows go into their pages.
+ *   pages  K, V and, for 8-bit pages, K_scale, V_scale are written as described
+ *   k_new, v_new  device kv_dtype [T,Hkv,d]
+ */
+int lrqk_pages_append(const lrqk_pages_shape* shape, const lrqk_pages* pages, const void* k_new,
+                      const void* v_new, void* stream);
+
+/*
+ * g2 — rows of the pages as dense arrays: for every sequence b and first <= p < kv_len[b],
+ *   K_out[b,kv,p,:] = the row of position p, V_out likewise; all other rows stay as they are.
+ * With first = the length before a chunk only that chunk's rows are brought up to date.
+ *   first >= 0
+ *   K_out, V_out  kv_dtype [B,Hkv,l_cap,d], device memory or pinned host memory; one of them may
+ *                 be NULL
+ */
+int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pages, int32_t first, void* K_out,
+                    void* V_out, void* stream);
+
+/*
+ * g3 — exact causal attention of the new tokens.  For token i of sequence b, at position
+ * p0 = kv_len[b] - n + i:
+ *   out[start[b]+i,h,:] = sum_{p <= p0} w_p V_p,   w = softmax_p(scale * q[start[b]+i,h,:] . K_p)
+ * over the positions that exist (their pages too), K and V of KV head h / G.  A token that sees no
+ * position, or only scores of -infinity, gets zeros.  What a token does not see does not reach its
+ * output, whatever its rows hold.  Products of bf16 operands are exact, sums fp32; with bf16 q the
+ * weights are rounded to bf16 before they meet V.
+ *   q    device kv_dtype [T,Hq,d]
+ *   out  device kv_dtype [T,Hq,d]  written
+ *   workspace  device, >= lrqk_pages_workspace_bytes(shape), 256-byte aligned
+ * The new tokens' own rows are read from their pages: lrqk_pages_append comes first, on the same
+ * stream.  LRQK_ENOMEM if ws_bytes is too small.
+ */
+int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* pages, const void* q, void* out,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Instrumentation (not part of the method): GPU time of the kernels of lrqk_decode_step, each
  * taken from a pair of HIP events attached to the kernel itself (they hold its own start and
  * end, so neither the gaps between launches nor the events' own cost are included).

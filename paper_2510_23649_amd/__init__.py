@@ -13,6 +13,9 @@ from .binding import (  # noqa: F401
     lrqk_cache_init, lrqk_cache_resolve, lrqk_calib_copy, lrqk_decode_step, lrqk_fetch_misses,
     lrqk_last_hip_error, lrqk_proxy_scores, lrqk_select_topk, lrqk_sparse_attend,
     lrqk_sparse_attend_noalloc,
+    LRQK_PAGE_BF16, LRQK_PAGE_E4M3, LRQK_PAGE_F32, LRQK_PAGE_I8, Pages, PagesShape, make_pages,
+    lrqk_chunk_attend, lrqk_pages_append, lrqk_pages_read, lrqk_pages_workspace_bytes,
+    lrqk_validate_pages,
     lrqk_status_string, lrqk_validate_shape, lrqk_version, lrqk_workspace_bytes, make_layer,
 )
 from .state import LayerBuffers  # noqa: F401

@@ -15,6 +15,7 @@ LRQK_KV_BF16, LRQK_KV_F32 = 0, 1
 LRQK_FETCH_STAGED, LRQK_FETCH_DIRECT, LRQK_FETCH_GROUP = 0, 1, 2
 LRQK_SELECT_FRESH = 0x100
 LRQK_WS_SELECT, LRQK_WS_ATTEND, LRQK_WS_UPDATE, LRQK_WS_PREFILL = 1, 2, 3, 4
+LRQK_PAGE_BF16, LRQK_PAGE_F32, LRQK_PAGE_E4M3, LRQK_PAGE_I8 = 0, 1, 2, 3
 
 
 class LrqkError(RuntimeError):
@@ -55,6 +56,24 @@ class Layer(C.Structure):
                                           "sel_thr")]
 
 
+class PagesShape(C.Structure):
+    """lrqk_pages_shape."""
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "T", "n_max", "l_max", "l_cap", "page",
+                                         "n_pages", "max_pages", "kv_dtype", "page_dtype")]
+    _fields_.append(("scale", C.c_float))
+
+    @classmethod
+    def make(cls, *, B, Hq, Hkv, T, n_max, l_max, page, n_pages, max_pages, d=128,
+             kv_dtype=LRQK_KV_BF16, page_dtype=LRQK_PAGE_BF16, scale=None, l_cap=0):
+        return cls(B, Hq, Hkv, d, T, n_max, l_max, l_cap, page, n_pages, max_pages, kv_dtype,
+                   page_dtype, float(scale if scale is not None else d ** -0.5))
+
+
+class Pages(C.Structure):
+    """lrqk_pages: raw pointers of a paged cache (make_pages keeps its tensors alive with it)."""
+    _fields_ = [(n, C.c_void_p) for n in ("K", "V", "K_scale", "V_scale", "table", "start", "kv_len")]
+
+
 class _StepDebug(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("sel_idx", "sel_slot", "hit", "miss_tok", "miss_slot",
                                           "n_miss", "link_rows")]
@@ -76,6 +95,7 @@ def load_library():
     lib = C.CDLL(_LIB_PATH)
     vp, i32, sz = C.c_void_p, C.c_int32, C.c_size_t
     sp = C.POINTER(Shape)
+    psp, pgp = C.POINTER(PagesShape), C.POINTER(Pages)
     sigs = {
         "lrqk_version": (C.c_int, []),
         "lrqk_status_string": (C.c_char_p, [C.c_int]),
@@ -94,6 +114,11 @@ def load_library():
         "lrqk_append_token": (C.c_int, [sp, C.POINTER(Layer), vp, vp, vp, vp]),
         "lrqk_prefill_factorize": (C.c_int, [sp, vp, vp, vp, vp, vp, vp, C.c_float, C.c_float,
                                              i32, vp, sz, vp]),
+        "lrqk_validate_pages": (C.c_int, [psp]),
+        "lrqk_pages_workspace_bytes": (sz, [psp]),
+        "lrqk_pages_append": (C.c_int, [psp, pgp, vp, vp, vp]),
+        "lrqk_pages_read": (C.c_int, [psp, pgp, i32, vp, vp, vp]),
+        "lrqk_chunk_attend": (C.c_int, [psp, pgp, vp, vp, vp, sz, vp]),
         "lrqk_plan_create": (C.c_int, [sp, C.POINTER(vp)]),
         "lrqk_plan_destroy": (C.c_int, [vp]),
         "lrqk_fetch_misses": (C.c_int, [vp, sp, vp, vp, vp, vp, vp, vp, vp, C.c_int,
@@ -118,7 +143,9 @@ EXPORTS = ["lrqk_version", "lrqk_status_string", "lrqk_last_hip_error", "lrqk_va
            "lrqk_cache_resolve", "lrqk_sparse_attend", "lrqk_plan_create", "lrqk_plan_destroy",
            "lrqk_fetch_misses", "lrqk_decode_step", "lrqk_plan_profile", "lrqk_plan_profile_read", "lrqk_calib_copy",
            "lrqk_plan_time_proxy_pass", "lrqk_factor_update", "lrqk_append_token",
-           "lrqk_prefill_factorize", "lrqk_sparse_attend_noalloc", "lrqk_select_state_init"]
+           "lrqk_prefill_factorize", "lrqk_sparse_attend_noalloc", "lrqk_select_state_init",
+           "lrqk_validate_pages", "lrqk_pages_workspace_bytes", "lrqk_pages_append",
+           "lrqk_pages_read", "lrqk_chunk_attend"]
 
 
 def _check(status: int, where: str):
@@ -333,3 +360,65 @@ def lrqk_decode_step(plan: Plan, shape, step, layer: Layer, q_hat, q, out,
         C.byref(dbg) if dbg is not None else None, C.byref(total), _stream(stream)),
         "lrqk_decode_step")
     return total.value
+
+
+def lrqk_validate_pages(shape: PagesShape) -> int:
+    return load_library().lrqk_validate_pages(C.byref(shape))
+
+
+def lrqk_pages_workspace_bytes(shape: PagesShape) -> int:
+    return load_library().lrqk_pages_workspace_bytes(C.byref(shape))
+
+
+_PAGE_TYPES = {torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.float8_e4m3fn}
+
+
+def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pages:
+    """8-bit rows may come as uint8, int8 or float8_e4m3fn: lrqk_pages_shape says what they hold."""
+    if K.dtype != V.dtype or K.dtype not in _PAGE_TYPES:
+        raise TypeError(f"pages of {K.dtype} and {V.dtype}")
+    p = Pages(_dev(K), _dev(V), _dev(K_scale, torch.uint8), _dev(V_scale, torch.uint8),
+              _dev(table, torch.int32), _dev(start, torch.int32), _dev(kv_len, torch.int32))
+    p.tensors = (K, V, K_scale, V_scale, table, start, kv_len)
+    return p
+
+
+def _fits(t: Optional[torch.Tensor], shape: PagesShape, rows: int, pinned=False):
+    """Pointer of a contiguous tensor of shape.kv_dtype with at least `rows` rows of d elements, on
+    the current device (or, with `pinned`, in pinned host memory)."""
+    if t is None:
+        return None
+    want = torch.bfloat16 if shape.kv_dtype == LRQK_KV_BF16 else torch.float32
+    if t.dtype != want:
+        raise TypeError(f"expected {want}, got {t.dtype}")
+    if t.numel() < rows * shape.d:
+        raise ValueError(f"expected {rows} rows of {shape.d}, got {tuple(t.shape)}")
+    if pinned and not t.is_cuda:
+        return _pinned(t)
+    ptr = _dev(t)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensor on {t.device}, current device is {torch.cuda.current_device()}")
+    return ptr
+
+
+def lrqk_pages_append(shape, pages, k_new, v_new, stream=None):
+    rows = shape.T * shape.Hkv
+    _check(load_library().lrqk_pages_append(C.byref(shape), C.byref(pages),
+                                            _fits(k_new, shape, rows), _fits(v_new, shape, rows),
+                                            _stream(stream)), "lrqk_pages_append")
+
+
+def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
+    rows = shape.B * shape.Hkv * (shape.l_cap if shape.l_cap > 0 else shape.l_max)
+    _check(load_library().lrqk_pages_read(C.byref(shape), C.byref(pages), int(first),
+                                          _fits(K_out, shape, rows, pinned=True),
+                                          _fits(V_out, shape, rows, pinned=True),
+                                          _stream(stream)), "lrqk_pages_read")
+
+
+def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
+    rows = shape.T * shape.Hq
+    _check(load_library().lrqk_chunk_attend(
+        C.byref(shape), C.byref(pages), _fits(q, shape, rows), _fits(out, shape, rows),
+        _dev(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+        "lrqk_chunk_attend")

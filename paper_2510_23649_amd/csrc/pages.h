@@ -1,0 +1,153 @@
+// Device helpers of the paged K/V cache: where a position lies, and rows held in 8 bits.
+#pragma once
+
+#include <type_traits>
+
+#include "lrqk_device.h"
+#include "lrqk_internal.h"
+
+namespace lrqk {
+
+int check_pages(const lrqk_pages_shape* s);
+// K, V, the scales that the type needs, table, start and kv_len: given and aligned.
+bool pages_given(const lrqk_pages_shape& s, const lrqk_pages* p);
+
+namespace pages {
+
+constexpr int kScaleBlock = 32;               // elements of a row that share a scale
+constexpr int kScales = kD / kScaleBlock;     // scale bytes of a row
+constexpr int kMinExp = -110;                 // smallest scale 2^e (include/lrqk.h)
+
+__host__ __device__ constexpr bool is8(int page_dtype) {
+  return page_dtype == LRQK_PAGE_E4M3 || page_dtype == LRQK_PAGE_I8;
+}
+__host__ __device__ constexpr int page_elem_bytes(int page_dtype) {
+  return page_dtype == LRQK_PAGE_F32 ? 4 : page_dtype == LRQK_PAGE_BF16 ? 2 : 1;
+}
+
+// The shape and the tables as the kernels take them.
+struct Map {
+  const int32_t* table;
+  const int32_t* start;
+  const int32_t* kv_len;
+  int B, Hkv, T, l_max, n_pages, max_pages, page_log2;
+};
+inline Map make_map(const lrqk_pages_shape& s, const lrqk_pages& p) {
+  return Map{p.table, p.start, p.kv_len, s.B,         s.Hkv,
+             s.T,     s.l_max, s.n_pages, s.max_pages, __builtin_ctz((unsigned)s.page)};
+}
+
+// Sequence b: its packed rows [first, first + n) and its length; position of row first + i: len - n + i.
+struct Seq {
+  int first, n, len;
+};
+__device__ __forceinline__ Seq sequence(const Map& m, int b) {
+  Seq q;
+  q.first = min(max(m.start[b], 0), m.T);
+  q.n = min(max(m.start[b + 1], q.first), m.T) - q.first;
+  q.len = max(m.kv_len[b], 0);
+  return q;
+}
+
+// Row (of d elements) of position p in [0, l_max) of sequence b for KV head kvh, or -1: no page.
+__device__ __forceinline__ int64_t row_of(const Map& m, int b, int kvh, int p) {
+  const int pg = m.table[(size_t)b * m.max_pages + (p >> m.page_log2)];
+  if ((unsigned)pg >= (unsigned)m.n_pages) return -1;
+  return ((((int64_t)pg * m.Hkv + kvh) << m.page_log2) + (p & ((1 << m.page_log2) - 1)));
+}
+
+// 2^(byte - 127); 255: NaN.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
+}
+
+// Eight codes (two dwords) times their scale, in fp32 (exact).
+template <int PAGE>
+__device__ __forceinline__ void decode8(uint2 c, float s, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w = i ? c.y : c.x;
+    if constexpr (PAGE == LRQK_PAGE_E4M3) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+      const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+      x[4 * i] = lo[0] * s;
+      x[4 * i + 1] = lo[1] * s;
+      x[4 * i + 2] = hi[0] * s;
+      x[4 * i + 3] = hi[1] * s;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[4 * i + j] = (float)(int8_t)(w >> (8 * j)) * s;
+    }
+  }
+}
+
+// The scale byte of a block whose largest magnitude has the bits `top` (compared as integers, so that
+// infinity and NaN win): the smallest e >= kMinExp with max <= 448 2^e or 127 2^e.  448 = 1.75 * 2^8,
+// 127 = 1.984375 * 2^6: one more where the mantissa is above theirs.
+template <int PAGE>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  constexpr int kTopExp = PAGE == LRQK_PAGE_E4M3 ? 8 : 6;
+  constexpr uint32_t kTopMant = PAGE == LRQK_PAGE_E4M3 ? 0x600000u : 0x7e0000u;
+  const int ex = (int)(top >> 23);
+  if (ex == 255) return 255u;
+  const int e = ex - 127 - kTopExp + ((top & 0x7fffffu) > kTopMant ? 1 : 0);
+  return (uint32_t)(max(e, kMinExp) + 127);
+}
+
+// Eight elements as codes of a block with that scale byte.
+template <int PAGE>
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], uint32_t byte) {
+  if (byte == 255u) return make_uint2(0u, 0u);
+  const float inv = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte), a normal number
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (PAGE == LRQK_PAGE_E4M3) {
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inv, x[4 * i + 1] * inv, 0, false);
+      v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inv, x[4 * i + 3] * inv, v, true);
+      w[i] = (uint32_t)v;
+    } else {
+      uint32_t v = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v |= ((uint32_t)(int)__builtin_rintf(x[4 * i + j] * inv) & 0xffu) << (8 * j);
+      w[i] = v;
+    }
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// Sequence that packed row t belongs to, or -1; the whole wavefront asks, each lane for its own t: the
+// starts are read once, 64 at a time, without a chain of dependent loads.
+__device__ __forceinline__ int sequence_of(const Map& m, int t) {
+  const int lane = threadIdx.x & 63;
+  int b = 0;
+  for (int i0 = 0; i0 < m.B; i0 += 64) {
+    const int e = i0 + lane < m.B ? m.start[i0 + lane + 1] : INT32_MAX;
+    const int todo = min(64, m.B - i0);
+    for (int j = 0; j < todo; ++j) b += __builtin_amdgcn_readlane(e, j) <= t ? 1 : 0;
+  }
+  return b < m.B && t >= m.start[0] && t < m.T ? b : -1;
+}
+
+// f(bf16 dense rows, page type) for the five combinations that check_pages lets through
+template <typename F>
+void by_type(const lrqk_pages_shape& s, F f) {
+  using std::integral_constant;
+  const bool bf16 = s.kv_dtype == LRQK_KV_BF16;
+  auto with = [&](auto page) {
+    if constexpr (page.value == LRQK_PAGE_BF16) f(std::true_type{}, page);
+    else if constexpr (page.value == LRQK_PAGE_F32) f(std::false_type{}, page);
+    else if (bf16) f(std::true_type{}, page);
+    else f(std::false_type{}, page);
+  };
+  switch (s.page_dtype) {
+    case LRQK_PAGE_BF16: with(integral_constant<int, LRQK_PAGE_BF16>{}); break;
+    case LRQK_PAGE_F32: with(integral_constant<int, LRQK_PAGE_F32>{}); break;
+    case LRQK_PAGE_E4M3: with(integral_constant<int, LRQK_PAGE_E4M3>{}); break;
+    default: with(integral_constant<int, LRQK_PAGE_I8>{}); break;
+  }
+}
+
+}  // namespace pages
+}  // namespace lrqk
