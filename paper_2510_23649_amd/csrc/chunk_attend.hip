@@ -1,8 +1,32 @@
 // g3 -- exact causal attention of new tokens over the paged cache (include/lrqk.h).
 //
-// One workgroup per (new token, query head).  16 lanes share a row of K and of V, 8 elements each; the
-// 16 groups of a workgroup take positions in turn, keep a running (max, sum, acc) each and merge at
-// the end.  Everything in fp32.
+// The query heads of a KV head attend to the same rows, so the n G (token, query head) pairs of a
+// sequence are the rows of one problem per KV head.  A wavefront holds 32 of them and makes
+//   S^T = K Q^T    (positions x rows)        O^T += V^T P^T    (elements x rows)
+// on the matrix cores.  With the positions as rows of the product, a lane has 16 scores of one row of
+// the problem in a register tile and lane + 32 the other 16: a row's maximum and sum are in-lane
+// operations and one exchange, and the exponentials are, register for register, the operand that the second
+// product takes, as long as it takes the positions in the order in which they lie there (register v, half h:
+// position 8 (v / 4) + 4 h + v % 4), which is how V is read from LDS, four positions at a time through the
+// transposing read.
+// One pass over the positions with a running maximum and sum.  The accumulators are only rescaled when
+// a row's maximum has grown by more than 2^kLag; until then weights up to 2^kLag are kept, which is
+// exact up to the rounding that the weights have anyway.
+//
+// Two shapes of workgroup, both of four wavefronts:
+//   tile  the wavefronts take 32 rows of the problem each and share the positions, 64 at a time (32
+//         in fp32) through two buffers in LDS: K and V are read once for 128 rows
+//   thin  at most 32 rows: each wavefront takes every fourth block of 32 positions through an LDS
+//         area of its own, without a barrier, and the four states are merged at the end
+// Rows are loaded into registers one block ahead (8-bit rows are decoded on the way into LDS, exactly:
+// a code times its scale is a bf16 number).
+//
+// V rows that a token does not see meet its weights as 0 * V, which is not 0 if V is not finite.
+// Positions that nobody sees are cleared; in blocks that some rows of the problem see and others do not,
+// elements that are not finite are cleared as well and added to the rows that see them at the end.
+#include <cmath>
+#include <algorithm>
+
 #include "pages.h"
 
 namespace lrqk {
@@ -11,7 +35,10 @@ namespace {
 using namespace pages;
 
 constexpr int kThreads = 256;
+constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLag = 8.0f;
+constexpr int kPartial = kPartialStride;  // floats of a partial state: max, sum, 2 unused, acc[128]
 
 struct Args {
   Map m;
@@ -19,75 +46,625 @@ struct Args {
   const uint8_t *K_scale, *V_scale;
   const void* q;
   void* out;
-  int Hq;
+  float* partials;  // [T*Hq][pieces][kPartial], or null: one piece, straight to out
+  int G, tiles, pieces, piece;
   float scale;
 };
 
-template <bool BF16, int PAGE>
-__device__ __forceinline__ void load_row8(const void* base, const uint8_t* sc, int64_t row, int c, float (&x)[8]) {
-  if constexpr (is8(PAGE)) {
-    decode8<PAGE>(static_cast<const uint2*>(base)[row * 16 + c], scale_of(sc[row * kScales + (c >> 2)]), x);
-  } else {
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+using dev::bf16x8;
+using dev::f32x16;
+
+// Row r of the problem of a sequence: token and query head within the group.
+struct Problem {
+  Seq s;
+  int b, r0, rows;  // first row of this workgroup, rows of the sequence
+};
+
+// The sequence and the first row of tile `tile` (M rows each), or b = -1.  Every wavefront finds it for
+// itself, 64 sequences at a time.
+template <int M>
+__device__ __forceinline__ Problem find_tile(const Args& a, int tile) {
+  const int lane = threadIdx.x & 63;
+  Problem p;
+  p.b = -1;
+  int before = 0;
+  for (int i0 = 0; i0 < a.m.B; i0 += 64) {
+    const int i = i0 + lane;
+    int tiles = 0;
+    if (i < a.m.B) {
+      const int lo = min(max(a.m.start[i], 0), a.m.T), hi = min(max(a.m.start[i + 1], lo), a.m.T);
+      tiles = ((hi - lo) * a.G + M - 1) / M;
+    }
+    const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)tiles);
+    const uint64_t past = __ballot(upto > tile);
+    if (past) {
+      const int j = __builtin_ctzll(past);
+      p.b = i0 + j;
+      const int mine = __builtin_amdgcn_readlane(upto, j) - __builtin_amdgcn_readlane(tiles, j);
+      p.s = sequence(a.m, p.b);
+      p.rows = p.s.n * a.G;
+      p.r0 = (tile - mine) * M;
+      return p;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return p;
+}
+
+// Positions that a row of the problem sees: [0, result).
+__device__ __forceinline__ int sees(const Args& a, const Problem& p, int row) {
+  return min(max(p.s.len - p.s.n + row / a.G + 1, 0), a.m.l_max);
+}
+
+// |scale| in units of log2 (its sign goes into q).  Never 0: a masked score is -infinity before it is scaled.
+__device__ __forceinline__ float log2_scale(const Args& a) { return fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f); }
+
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A dword of V (two bf16 or one fp32): an infinity or a NaN in it; the same without them.
+template <bool BF16>
+__device__ __forceinline__ bool odd(uint32_t w) {
+  return (w & 0x7f800000u) == 0x7f800000u || (BF16 && (w & 0x7f80u) == 0x7f80u);
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t clear(uint32_t w) {
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= BF16 ? 0xffffu : 0u;
+  if (BF16 && (w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  return w;
+}
+
+// ---- a block of rows on its way from the pages through registers into LDS ------------------------------
+// ROWS rows by NW wavefronts; wavefront w takes rows w ROWS / NW and on.  LDS rows of kRowB bytes in
+// 16-byte chunks, their order within a row turned by a mask that depends on the row, so that neither the reads of K (32 rows,
+// one chunk each) nor those of V (8 rows, 32 bytes each) fall on the same banks.
+template <bool BF16>
+constexpr int kRowB = kD * (BF16 ? 2 : 4);
+template <bool BF16>
+__device__ __forceinline__ int k_chunk(int row, int c) {
+  return row * kRowB<BF16> + ((c ^ (row & 15)) << 4);
+}
+__device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ ((row & 7) << 1)) << 4); }
+
+template <bool BF16, int PAGE, int ROWS, int NW>
+struct Block {
+  static constexpr int kLoad = is8(PAGE) || BF16 ? 16 : 32;               // bytes a lane loads of a row
+  static constexpr int kLanes = kD * page_elem_bytes(PAGE) / kLoad;       // lanes a row
+  static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
+  static constexpr int kN = ROWS / NW / kPass;                            // such loads
+  static constexpr int kRegs = kLoad / 16;
+  uint4 k[kN][kRegs], v[kN][kRegs];
+  uint32_t ks[kN], vs[kN];
+  int pg[kN];       // page of each of the lane's rows, one block ahead
+  uint32_t there;   // bit of each of the wavefront's rows
+
+  static __device__ __forceinline__ int row_in_wave(int i, int lane) { return i * kPass + lane / kLanes; }
+
+  // table entries for the block at position p0; end: first position that is none
+  __device__ __forceinline__ void look_up(const Map& m, int b, int p0, int end, int w, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(base)[row * kD + 8 * c + i] << 16)
-                  : static_cast<const float*>(base)[row * kD + 8 * c + i];
+    for (int i = 0; i < kN; ++i) {
+      const int p = p0 + w * (ROWS / NW) + row_in_wave(i, lane);
+      pg[i] = m.table[(size_t)b * m.max_pages + (min(p, end - 1) >> m.page_log2)];
+    }
+  }
+
+  // rows of the block at p0, whose pages have been looked up; what is not there reads row 0
+  __device__ __forceinline__ void load(const Args& a, int kvh, int p0, int end, int w, int lane) {
+    there = 0;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int p = p0 + w * (ROWS / NW) + row_in_wave(i, lane);
+      const bool ok = p < end && (unsigned)pg[i] < (unsigned)a.m.n_pages;
+      const int64_t at = ((((int64_t)pg[i] * a.m.Hkv + kvh) << a.m.page_log2) + (p & ((1 << a.m.page_log2) - 1)));
+      const int64_t row = ok ? at : 0;
+      const uint64_t vote = __ballot(ok);
+#pragma unroll
+      for (int j = 0; j < kPass; ++j) there |= (uint32_t)((vote >> (j * kLanes)) & 1) << (i * kPass + j);
+      const int c = lane % kLanes;
+#pragma unroll
+      for (int j = 0; j < kRegs; ++j) {
+        k[i][j] = static_cast<const uint4*>(a.K)[(row * kLanes + c) * kRegs + j];
+        v[i][j] = static_cast<const uint4*>(a.V)[(row * kLanes + c) * kRegs + j];
+      }
+      if constexpr (is8(PAGE)) {  // 16 codes: half a scale block
+        ks[i] = a.K_scale[row * kScales + (c >> 1)];
+        vs[i] = a.V_scale[row * kScales + (c >> 1)];
+      }
+    }
+  }
+
+  // 16-byte chunks of the LDS row that a lane's load makes, and where the first of them goes
+  static constexpr int kOut = kRowB<BF16> / 16 / kLanes;
+  static __device__ __forceinline__ void widen(const uint4 (&x)[kRegs], uint32_t byte, uint4 (&o)[kOut]) {
+    if constexpr (!is8(PAGE)) {
+#pragma unroll
+      for (int j = 0; j < kOut; ++j) o[j] = x[j];
+    } else {
+      const float s = scale_of(byte);
+      const uint32_t w[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float f[8];
+        decode8<PAGE>(make_uint2(w[2 * j], w[2 * j + 1]), s, f);
+        if constexpr (BF16) {
+          o[j] = make_uint4(dev::pack_bf16(f[0], f[1]), dev::pack_bf16(f[2], f[3]), dev::pack_bf16(f[4], f[5]),
+                            dev::pack_bf16(f[6], f[7]));
+        } else {
+          o[2 * j] = __builtin_bit_cast(uint4, f32x4{f[0], f[1], f[2], f[3]});
+          o[2 * j + 1] = __builtin_bit_cast(uint4, f32x4{f[4], f[5], f[6], f[7]});
+        }
+      }
+    }
+  }
+
+  // into LDS; part: some rows of the problem see the block and others do not.  Returns whether elements of V were left
+  // out for that.
+  __device__ __forceinline__ bool store(char* kt, char* vt, bool part, int w, int lane) const {
+    constexpr uint32_t kAll = ROWS / NW == 32 ? 0xffffffffu : (1u << (ROWS / NW)) - 1u;
+    bool left_out = false;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int in_wave = row_in_wave(i, lane), row = w * (ROWS / NW) + in_wave, c = (lane % kLanes) * kOut;
+      uint4 ko[kOut], vo[kOut];
+      widen(k[i], is8(PAGE) ? ks[i] : 0u, ko);
+      widen(v[i], is8(PAGE) ? vs[i] : 0u, vo);
+      if (there != kAll && !((there >> in_wave) & 1)) {
+#pragma unroll
+        for (int j = 0; j < kOut; ++j) vo[j] = make_uint4(0, 0, 0, 0);
+      }
+      if (part) {
+#pragma unroll
+        for (int j = 0; j < kOut; ++j) {
+          left_out |= odd<BF16>(vo[j].x) || odd<BF16>(vo[j].y) || odd<BF16>(vo[j].z) || odd<BF16>(vo[j].w);
+          vo[j] = make_uint4(clear<BF16>(vo[j].x), clear<BF16>(vo[j].y), clear<BF16>(vo[j].z), clear<BF16>(vo[j].w));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kOut; ++j) {
+        *reinterpret_cast<uint4*>(kt + k_chunk<BF16>(row, c + j)) = ko[j];
+        *reinterpret_cast<uint4*>(vt + (BF16 ? v_chunk(row, c + j) : row * kRowB<false> + ((c + j) << 4))) = vo[j];
+      }
+    }
+    return left_out;
+  }
+};
+
+// ---- 32 rows of the problem in a wavefront ---------------------------------------------------------------
+// Lane l: row l % 32; element e of S^T or O^T: dev::mfma_row(e, l).
+template <bool BF16>
+struct Rows {
+  uint4 q[BF16 ? 8 : 16];  // bf16: elements 16 s + 8 h .. + 7; fp32: 8 s + 4 h .. + 3
+  f32x16 o[4];             // elements 32 t .. of O^T
+  float mx, sum;           // of what has been seen, in units of log2
+  int see;                 // positions that the lane's row sees
+
+  __device__ __forceinline__ void start(const void* base, int64_t row, bool negate, int lane) {
+    const int h = lane >> 5;
+    const uint32_t flip = negate ? (BF16 ? 0x80008000u : 0x80000000u) : 0u;
+#pragma unroll
+    for (int s = 0; s < (BF16 ? 8 : 16); ++s) {
+      uint4 x = static_cast<const uint4*>(base)[row * (kRowB<BF16> / 16) + 2 * s + h];
+      x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+      q[s] = x;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+    mx = -INFINITY;
+    sum = 0.0f;
+  }
+
+  // NS blocks of 32 positions from p0 in LDS, rows `there`; c: scale in log2
+  template <int NS>
+  __device__ __forceinline__ void attend(const char* kt, const char* vt, int p0, uint64_t there, bool all_see,
+                                         float c, int lane) {
+    const int h = lane >> 5, i = lane & 31;
+    f32x16 s[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
+    if constexpr (BF16) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+          s[n] = dev::mfma_bf16(
+              __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kt + k_chunk<true>(32 * n + i, 2 * k + h))),
+              __builtin_bit_cast(bf16x8, q[k]), s[n]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(kt + k_chunk<false>(32 * n + i, 2 * k + h));
+          const f32x4 y = __builtin_bit_cast(f32x4, q[k]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], s[n], 0, 0, 0);
+        }
+    }
+    constexpr uint64_t kAll = NS == 2 ? ~0ull : 0xffffffffull;
+    if (!(all_see && there == kAll)) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int p = 32 * n + dev::mfma_row(e, lane);
+          const bool ok = p0 + p < see && ((there >> p) & 1);
+          s[n][e] = ok ? s[n][e] : -INFINITY;
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
+    top = max_halves(top) * c;
+    if (__any(top > mx + kLag)) {
+      const float to = fmaxf(mx, top);
+      const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mx - to);
+      sum *= f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] *= f;
+      mx = to;
+    }
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float add = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -base));
+        add += s[n][e];
+      }
+    sum += add;
+    if constexpr (BF16) {
+      const int g = lane & 15;
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint4 pw = make_uint4(dev::pack_bf16(s[n][8 * k], s[n][8 * k + 1]),
+                                      dev::pack_bf16(s[n][8 * k + 2], s[n][8 * k + 3]),
+                                      dev::pack_bf16(s[n][8 * k + 4], s[n][8 * k + 5]),
+                                      dev::pack_bf16(s[n][8 * k + 6], s[n][8 * k + 7]));
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            // a transposing read: the 16 lanes of a group point at 4 rows of 16 elements, lane g gets column g
+            s16x4 x[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int row = 32 * n + 16 * k + 8 * j + 4 * h + (g >> 2);
+              const int chunk = 4 * t + 2 * ((lane >> 4) & 1) + ((g & 3) >> 1);
+              x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) s16x4*)(vt + v_chunk(row, chunk) + 8 * (g & 1)));
+            }
+            const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            o[t] = dev::mfma_bf16(v, __builtin_bit_cast(bf16x8, pw), o[t]);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float* row = reinterpret_cast<const float*>(vt + (32 * n + dev::mfma_row(e, lane)) * kRowB<false>);
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[32 * t + i], s[n][e], o[t], 0, 0, 0);
+        }
+    }
+  }
+};
+
+// Four consecutive elements of a row of the output, or of a partial state (the row's max and sum with element 0).
+template <bool BF16>
+__device__ __forceinline__ void put(const Args& a, const Problem& p, int kvh, int row, int piece, int e0, f32x4 x,
+                                    float mx, float sum) {
+  const int t = p.s.first + row / a.G, h = kvh * a.G + row % a.G;
+  const int64_t at = (int64_t)t * (a.m.Hkv * a.G) + h;
+  if (a.partials) {
+    float* P = a.partials + (at * a.pieces + piece) * kPartial;
+    *reinterpret_cast<f32x4*>(P + 4 + e0) = x;
+    if (e0 == 0) {
+      P[0] = mx;
+      P[1] = sum;
+    }
+    return;
+  }
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = sum == 0.0f ? 0.0f : x[e] * f;
+  if constexpr (BF16)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * kD + e0) =
+        make_uint2(dev::pack_bf16(x[0], x[1]), dev::pack_bf16(x[2], x[3]));
+  else
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at * kD + e0) = x;
+}
+
+// Elements of V that are not finite at positions [from, to) that some rows of the workgroup see and others do not were left
+// out: each row gets those that it sees, a thread per element.  Rare, and slow.
+template <bool BF16, int PAGE>
+__device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows, int piece, int from, int to) {
+  __syncthreads();  // what this workgroup has written is read below
+  const int d = threadIdx.x % kD;
+  for (int r = threadIdx.x / kD; r < rows; r += kThreads / kD) {
+    const int row = p.r0 + r, end = min(to, sees(a, p, row));
+    float x = 0.0f;
+    for (int pos = from; pos < end; ++pos) {
+      const int64_t at = row_of(a.m, p.b, kvh, pos);
+      if (at < 0) continue;
+      float v;
+      if constexpr (is8(PAGE)) {
+        v = a.V_scale[at * kScales + d / kScaleBlock] == 255 ? NAN : 0.0f;
+      } else if constexpr (PAGE == LRQK_PAGE_BF16) {
+        v = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.V)[at * kD + d] << 16);
+      } else {
+        v = static_cast<const float*>(a.V)[at * kD + d];
+      }
+      if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) x += v;
+    }
+    if (x == 0.0f) continue;
+    const int64_t at = (int64_t)(p.s.first + row / a.G) * (a.m.Hkv * a.G) + kvh * a.G + row % a.G;
+    if (a.partials) a.partials[(at * a.pieces + piece) * kPartial + 4 + d] += x;
+    else if (BF16) {
+      __bf16* o = static_cast<__bf16*>(a.out) + at * kD + d;
+      *o = (__bf16)((float)*o + x);
+    } else {
+      static_cast<float*>(a.out)[at * kD + d] += x;
+    }
   }
 }
 
+// Workgroups: KV head fastest (its rows stay in one die's L2), then tile, last tiles first: they are the longest.
+struct Unit {
+  int kvh, tile, piece;
+};
+__device__ __forceinline__ Unit unit_of(const Args& a, int i) {
+  Unit u;
+  u.kvh = i % a.m.Hkv;
+  const int j = i / a.m.Hkv;
+  u.tile = a.tiles - 1 - j % a.tiles;
+  u.piece = j / a.tiles;
+  return u;
+}
+
 template <bool BF16, int PAGE>
-__global__ __launch_bounds__(kThreads) void chunk_attend_kernel(const Args a) {
-  __shared__ float gm[16], gs[16], gacc[16][kD];
-  const Map& m = a.m;
-  const int t = blockIdx.x, h = blockIdx.y, grp = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const int kvh = h / (a.Hq / m.Hkv);
-  const int b = sequence_of(m, t);
-  if (b < 0) return;
-  const Seq s = sequence(m, b);
-  if (t < s.first || t >= s.first + s.n) return;
-  const int see = min(max(s.len - s.n + (t - s.first) + 1, 0), m.l_max);
-  float q[8];
-  load_row8<BF16, BF16 ? LRQK_PAGE_BF16 : LRQK_PAGE_F32>(a.q, nullptr, (int64_t)t * a.Hq + h, c, q);
-  float mx = -INFINITY, sum = 0.0f, acc[8] = {};
-  for (int p = grp; p < see; p += 16) {
-    const int64_t row = row_of(m, b, kvh, p);
-    if (row < 0) continue;
-    float x[8], d = 0.0f;
-    load_row8<BF16, PAGE>(a.K, a.K_scale, row, c, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) d = __builtin_fmaf(q[i], x[i], d);
-#pragma unroll
-    for (int i = 1; i < 16; i <<= 1) d += __shfl_xor(d, i);
-    d *= a.scale * kLog2e;
-    const float mn = fmaxf(mx, d);
-    if (mn == -INFINITY) continue;
-    const float f = exp2f(mx - mn), w = exp2f(d - mn);
-    load_row8<BF16, PAGE>(a.V, a.V_scale, row, c, x);
-    sum = sum * f + w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(w, x[i], acc[i] * f);
-    mx = d != d ? d : mn;
-  }
-  if (c == 0) {
-    gm[grp] = mx;
-    gs[grp] = sum;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) gacc[grp][8 * c + i] = acc[i];
-  __syncthreads();
-  if (threadIdx.x >= kD) return;
-  float M = -INFINITY, S = 0.0f, A = 0.0f;
-  for (int i = 0; i < 16; ++i) M = gm[i] != gm[i] ? gm[i] : fmaxf(M, gm[i]);
-  for (int i = 0; i < 16; ++i)
-    if (gm[i] != -INFINITY) {
-      const float f = exp2f(gm[i] - M);
-      S += gs[i] * f;
-      A += gacc[i][threadIdx.x] * f;
+__global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
+  constexpr int NS = BF16 ? 2 : 1, BN = 32 * NS, M = 128;
+  constexpr int kTile = BN * kRowB<BF16>;
+  __shared__ __align__(16) char kt[2][kTile], vt[2][kTile];
+  __shared__ __align__(8) uint16_t there[2][4];
+  __shared__ int left_out;
+  const Unit u = unit_of(a, blockIdx.x);
+  const Problem p = find_tile<M>(a, u.tile);
+  if (p.b < 0) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = min(M, p.rows - p.r0);
+  const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
+  const int from = u.piece * a.piece, end = min(most, from + a.piece);
+  if (from >= end && u.piece > 0) return;  // (piece 0 writes the rows that see nothing)
+  const int mine = p.r0 + w * 32 + (lane & 31);  // rows behind the last repeat it
+  Rows<BF16> r;
+  const int real = min(mine, p.rows - 1);
+  r.see = sees(a, p, real);
+  r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+  const bool busy = p.r0 + w * 32 < p.rows;
+  const int my_least = sees(a, p, min(p.r0 + w * 32, p.rows - 1));
+  const int my_most = sees(a, p, min(p.r0 + w * 32 + 31, p.rows - 1));
+  const float c = log2_scale(a);
+  if (threadIdx.x == 0) left_out = 0;
+  if (from < end) {
+    Block<BF16, PAGE, BN, kWaves> blk;
+    blk.look_up(a.m, p.b, from, end, w, lane);
+    blk.load(a, u.kvh, from, end, w, lane);
+    blk.look_up(a.m, p.b, from + BN, end, w, lane);
+    bool cleared = false;
+    int buf = 0;
+    for (int p0 = from; p0 < end; p0 += BN, buf ^= 1) {
+      cleared |= blk.store(kt[buf], vt[buf], p0 + BN > least, w, lane);
+      if (lane == 0) there[buf][w] = (uint16_t)blk.there;
+      __syncthreads();
+      if (p0 + BN < end) {
+        blk.load(a, u.kvh, p0 + BN, end, w, lane);
+        blk.look_up(a.m, p.b, p0 + 2 * BN, end, w, lane);
+      }
+      if (busy && p0 < my_most) {
+        uint64_t bits;
+        if constexpr (BF16) {
+          bits = *reinterpret_cast<const uint64_t*>(there[buf]);
+        } else {
+          bits = there[buf][0] | there[buf][1] << 8 | there[buf][2] << 16 | (uint64_t)there[buf][3] << 24;
+        }
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)bits);
+        const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(bits >> 32));
+        r.template attend<NS>(kt[buf], vt[buf], p0, (uint64_t)hi << 32 | lo, p0 + BN <= my_least, c, lane);
+      }
     }
-  const float y = S == 0.0f ? 0.0f : A / S;
-  const size_t at = ((size_t)t * a.Hq + h) * kD + threadIdx.x;
-  if (BF16) static_cast<__bf16*>(a.out)[at] = (__bf16)y;
-  else static_cast<float*>(a.out)[at] = y;
+    if (cleared) left_out = 1;
+  }
+  r.sum = sum_halves(r.sum);
+  if (mine < p.rows) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put<BF16>(a, p, u.kvh, mine, u.piece, 32 * t + 8 * e + 4 * (lane >> 5),
+                  f32x4{r.o[t][4 * e], r.o[t][4 * e + 1], r.o[t][4 * e + 2], r.o[t][4 * e + 3]}, r.mx, r.sum);
+  }
+  __syncthreads();
+  if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
+}
+
+template <bool BF16, int PAGE>
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(const Args a) {
+  constexpr int M = 32, BN = 32;
+  constexpr int kTile = BN * kRowB<BF16>;
+  extern __shared__ __align__(16) char lds[];  // per wavefront: K, V
+  __shared__ float wm[kWaves][M], ws[kWaves][M];
+  __shared__ int left_out;
+  const Unit u = unit_of(a, blockIdx.x);
+  const Problem p = find_tile<M>(a, u.tile);
+  if (p.b < 0) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = min(M, p.rows - p.r0);
+  const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
+  const int from = u.piece * a.piece, end = min(most, from + a.piece);
+  if (from >= end && u.piece > 0) return;
+  Rows<BF16> r;
+  const int real = min(p.r0 + (lane & 31), p.rows - 1);
+  r.see = sees(a, p, real);
+  r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+  const float c = log2_scale(a);
+  if (threadIdx.x == 0) left_out = 0;
+  char* const kt = lds + w * 2 * kTile;
+  char* const vt = kt + kTile;
+  bool cleared = false;
+  const int mine = from + w * BN;
+  if (mine < end) {
+    Block<BF16, PAGE, BN, 1> blk;
+    blk.look_up(a.m, p.b, mine, end, 0, lane);
+    blk.load(a, u.kvh, mine, end, 0, lane);
+    blk.look_up(a.m, p.b, mine + kWaves * BN, end, 0, lane);
+    for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
+      __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
+      cleared |= blk.store(kt, vt, p0 + BN > least, 0, lane);
+      __builtin_amdgcn_wave_barrier();
+      const uint32_t there = blk.there;
+      if (p0 + kWaves * BN < end) {
+        blk.load(a, u.kvh, p0 + kWaves * BN, end, 0, lane);
+        blk.look_up(a.m, p.b, p0 + 2 * kWaves * BN, end, 0, lane);
+      }
+      r.template attend<1>(kt, vt, p0, there, p0 + BN <= least, c, lane);
+    }
+  }
+  // merge the four states: the accumulators, at a common maximum, meet in LDS
+  r.sum = sum_halves(r.sum);
+  if (lane < M) {
+    wm[w][lane] = r.mx;
+    ws[w][lane] = r.sum;
+  }
+  __syncthreads();
+  if (cleared) left_out = 1;
+  const int i = lane & 31, h = lane >> 5;
+  const float top = fmaxf(fmaxf(wm[0][i], wm[1][i]), fmaxf(wm[2][i], wm[3][i]));
+  const float f = r.mx == -INFINITY ? (r.sum == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(r.mx - top);
+  float* const acc = reinterpret_cast<float*>(lds);  // [wave][row][128], 16-byte chunks turned by the row
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4*>(acc + (w * M + i) * kD + 4 * ((8 * t + 2 * e + h) ^ i)) =
+          f32x4{r.o[t][4 * e] * f, r.o[t][4 * e + 1] * f, r.o[t][4 * e + 2] * f, r.o[t][4 * e + 3] * f};
+  __syncthreads();
+  for (int j = threadIdx.x; j < rows * (kD / 4); j += kThreads) {
+    const int row = j / (kD / 4), chunk = j % (kD / 4);
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    float mx = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, wm[v][row]);
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      const float g = wm[v][row] == -INFINITY ? (ws[v][row] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(wm[v][row] - mx);
+      sum += ws[v][row] * g;
+      x += *reinterpret_cast<const f32x4*>(acc + (v * M + row) * kD + 4 * (chunk ^ row));
+    }
+    put<BF16>(a, p, u.kvh, p.r0 + row, u.piece, 4 * chunk, x, mx, sum);
+  }
+  __syncthreads();
+  if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
+}
+
+// The pieces of a row's context joined: a wavefront per row, two elements a lane.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int64_t n_rows) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int Hq = a.m.Hkv * a.G;
+  const int t = (int)min(at / Hq, (int64_t)a.m.T);
+  const int b = sequence_of(a.m, t);
+  if (at >= n_rows || b < 0) return;
+  const Seq s = sequence(a.m, b);
+  if (t < s.first || t >= s.first + s.n) return;
+  const int see = min(max(s.len - s.n + (t - s.first) + 1, 0), a.m.l_max);
+  const int pieces = max(1, (see + a.piece - 1) / a.piece);
+  const float* P = a.partials + at * a.pieces * kPartial;
+  float mx = -INFINITY, sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
+  for (int i = 0; i < pieces; ++i) mx = fmaxf(mx, P[(int64_t)i * kPartial]);
+  for (int i = 0; i < pieces; ++i) {
+    const float* p = P + (int64_t)i * kPartial;
+    const float f = p[0] == -INFINITY ? (p[1] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(p[0] - mx);
+    sum += p[1] * f;
+    x0 += p[4 + 2 * lane] * f;
+    x1 += p[5 + 2 * lane] * f;
+  }
+  x0 = sum == 0.0f ? 0.0f : x0 / sum;
+  x1 = sum == 0.0f ? 0.0f : x1 / sum;
+  if constexpr (BF16) static_cast<uint32_t*>(a.out)[at * (kD / 2) + lane] = dev::pack_bf16(x0, x1);
+  else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
+}
+
+// How a call is cut up.  thin: at most 32 rows a sequence and KV head.  The context of a tile is cut into
+// pieces where there are too few tiles to fill 256 compute units with two workgroups each.
+struct Cut {
+  bool thin;
+  int tiles, pieces, piece;
+};
+Cut cut(const lrqk_pages_shape& s) {
+  const int G = s.Hq / s.Hkv;
+  Cut c;
+  c.thin = (int64_t)s.n_max * G <= 32;
+  const int M = c.thin ? 32 : 128;
+  c.tiles = (int)(((int64_t)s.T * G + M - 1) / M) + s.B;  // no fewer than sum_b ceil(n_b G / M)
+  const int64_t units = std::max<int64_t>(1, std::max<int64_t>(s.B, ((int64_t)s.T * G + M - 1) / M)) * s.Hkv;
+  const int least = c.thin ? 256 : 1024;
+  const int64_t want = c.thin ? 1024 : 512;
+  int64_t pieces = (want + units - 1) / units;
+  int64_t piece = (s.l_max + pieces - 1) / pieces;
+  piece = std::max<int64_t>(piece, least);
+  piece = (piece + 127) / 128 * 128;
+  c.piece = (int)piece;
+  c.pieces = (int)((s.l_max + piece - 1) / piece);
+  return c;
+}
+size_t partial_bytes(const lrqk_pages_shape& s) {
+  const Cut c = cut(s);
+  return c.pieces > 1 ? (size_t)s.T * s.Hq * c.pieces * kPartial * sizeof(float) : 0;
+}
+
+template <bool BF16, int PAGE>
+hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)c.tiles * s.Hkv * c.pieces));
+  if (c.thin) {
+    constexpr size_t kLds = (size_t)kWaves * 2 * 32 * kRowB<BF16>;
+    static std::atomic<uint64_t> done{0};
+    if (kLds > 65536 - 2048) {
+      const hipError_t e = raise_dynamic_lds_once(attend_thin_kernel<BF16, PAGE>, kLds, done);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((attend_thin_kernel<BF16, PAGE>), grid, dim3(kThreads), kLds, st, a);
+  } else {
+    hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
+  }
+  if (a.partials) {
+    const int64_t rows = (int64_t)s.T * s.Hq;
+    hipLaunchKernelGGL((attend_join_kernel<BF16>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
+                       a, rows);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -96,7 +673,9 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_kernel(const Args a) {
 #define LRQK_API extern "C" __attribute__((visibility("default")))
 
 LRQK_API size_t lrqk_pages_workspace_bytes(const lrqk_pages_shape* shape) {
-  return lrqk::check_pages(shape) == LRQK_OK ? 256 : 0;
+  using namespace lrqk;
+  if (check_pages(shape) != LRQK_OK) return 0;
+  return std::max<size_t>(256, partial_bytes(*shape));
 }
 
 LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* pg, const void* q, void* out,
@@ -108,11 +687,14 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   if (!pages_given(s, pg) || !q || !out || !aligned16(q) || !aligned16(out)) return LRQK_EINVAL;
   if (!workspace || !aligned256(workspace)) return LRQK_EINVAL;
   if (ws_bytes < lrqk_pages_workspace_bytes(shape)) return LRQK_ENOMEM;
-  const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out, s.Hq, s.scale};
+  const Cut c = cut(s);
+  const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
+               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.tiles, c.pieces, c.piece,
+               s.scale};
+  hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {
-    hipLaunchKernelGGL((chunk_attend_kernel<bf16.value, page.value>), dim3(s.T, s.Hq), dim3(kThreads), 0,
-                       static_cast<hipStream_t>(stream), a);
+    e = launch<bf16.value, page.value>(s, c, a, static_cast<hipStream_t>(stream));
   });
-  LRQK_HIP(hipGetLastError());
+  LRQK_HIP(e);
   return LRQK_OK;
 }
