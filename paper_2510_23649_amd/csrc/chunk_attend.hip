@@ -48,6 +48,7 @@ struct Args {
   void* out;
   float* partials;  // [T*Hq][pieces][kPartial], or null: one piece, straight to out
   int G, tiles, pieces, piece;
+  uint32_t page16;  // 16-byte chunks of a page (of all KV heads)
   float scale;
 };
 
@@ -135,52 +136,90 @@ __device__ __forceinline__ int k_chunk(int row, int c) {
 }
 __device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ ((row & 7) << 1)) << 4); }
 
-template <bool BF16, int PAGE, int ROWS, int NW>
+template <bool BF16, int PAGE, int ROWS, int NW, int LOAD = 16>
 struct Block {
-  static constexpr int kLoad = is8(PAGE) || BF16 ? 16 : 32;               // bytes a lane loads of a row
+  static constexpr int kLoad = LOAD;                                      // bytes a lane loads of a row
   static constexpr int kLanes = kD * page_elem_bytes(PAGE) / kLoad;       // lanes a row
   static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
   static constexpr int kN = ROWS / NW / kPass;                            // such loads
   static constexpr int kRegs = kLoad / 16;
+  static constexpr uint32_t kAll = ROWS / NW == 32 ? 0xffffffffu : (1u << (ROWS / NW)) - 1u;
   uint4 k[kN][kRegs], v[kN][kRegs];
   uint32_t ks[kN], vs[kN];
   int pg[kN];       // page of each of the lane's rows, one block ahead
+  uint64_t at[kN];  // first 16-byte chunk of each of the lane's rows in the pool; 0 where there is none
   uint32_t there;   // bit of each of the wavefront's rows
 
   static __device__ __forceinline__ int row_in_wave(int i, int lane) { return i * kPass + lane / kLanes; }
 
   // table entries for the block at position p0; end: first position that is none
   __device__ __forceinline__ void look_up(const Map& m, int b, int p0, int end, int w, int lane) {
+    const int32_t* table = m.table + (size_t)b * m.max_pages;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int p = p0 + w * (ROWS / NW) + row_in_wave(i, lane);
-      pg[i] = m.table[(size_t)b * m.max_pages + (min(p, end - 1) >> m.page_log2)];
+      pg[i] = table[(uint32_t)min(p, end - 1) >> m.page_log2];
     }
   }
 
-  // rows of the block at p0, whose pages have been looked up; what is not there reads row 0
-  __device__ __forceinline__ void load(const Args& a, int kvh, int p0, int end, int w, int lane) {
-    there = 0;
+  // rows of the block at p0, whose pages have been looked up
+  __device__ __forceinline__ void find(const Args& a, int kvh, int p0, int end, int w, int lane) {
+    constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;
+    const uint32_t head = ((uint32_t)kvh << a.m.page_log2) * kRow16, in_page = (1u << a.m.page_log2) - 1;
+    bool ok[kN], all = true;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int p = p0 + w * (ROWS / NW) + row_in_wave(i, lane);
-      const bool ok = p < end && (unsigned)pg[i] < (unsigned)a.m.n_pages;
-      const int64_t at = ((((int64_t)pg[i] * a.m.Hkv + kvh) << a.m.page_log2) + (p & ((1 << a.m.page_log2) - 1)));
-      const int64_t row = ok ? at : 0;
-      const uint64_t vote = __ballot(ok);
+      const uint32_t p = (uint32_t)(p0 + w * (ROWS / NW) + row_in_wave(i, lane));
+      ok[i] = ((int)p < end) & ((uint32_t)pg[i] < (uint32_t)a.m.n_pages);
+      all &= ok[i];
+      const uint64_t x = (uint64_t)(uint32_t)pg[i] * a.page16 + (head + (p & in_page) * kRow16);
+      at[i] = ok[i] ? x : 0;
+    }
+    there = kAll;
+    if (__builtin_expect(__ballot(all) != ~0ull, 0)) {
+      asm volatile("");  // a branch: taken by few blocks
+      there = 0;
 #pragma unroll
-      for (int j = 0; j < kPass; ++j) there |= (uint32_t)((vote >> (j * kLanes)) & 1) << (i * kPass + j);
-      const int c = lane % kLanes;
+      for (int i = 0; i < kN; ++i) {
+        const uint64_t v = __ballot(ok[i]);
 #pragma unroll
-      for (int j = 0; j < kRegs; ++j) {
-        k[i][j] = static_cast<const uint4*>(a.K)[(row * kLanes + c) * kRegs + j];
-        v[i][j] = static_cast<const uint4*>(a.V)[(row * kLanes + c) * kRegs + j];
-      }
-      if constexpr (is8(PAGE)) {  // 16 codes: half a scale block
-        ks[i] = a.K_scale[row * kScales + (c >> 1)];
-        vs[i] = a.V_scale[row * kScales + (c >> 1)];
+        for (int j = 0; j < kPass; ++j) there |= (uint32_t)((v >> (j * kLanes)) & 1) << (i * kPass + j);
       }
     }
+  }
+
+  // the rows found, into registers; what is not there reads row 0
+  __device__ __forceinline__ void load(const Args& a, int lane) {
+    const int c = lane % kLanes;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+#pragma unroll
+      for (int j = 0; j < kRegs; ++j) {
+        k[i][j] = static_cast<const uint4*>(a.K)[at[i] + c * kRegs + j];
+        v[i][j] = static_cast<const uint4*>(a.V)[at[i] + c * kRegs + j];
+      }
+      if constexpr (is8(PAGE)) {  // 16 codes: half a scale block; a row has 8 chunks and 4 scales
+        ks[i] = a.K_scale[(at[i] + c) >> 1];
+        vs[i] = a.V_scale[(at[i] + c) >> 1];
+      }
+    }
+  }
+
+  // the rows found, all of them there and of the type that LDS holds, straight into LDS: a wavefront's load fills 1 KB,
+  // 16 bytes a lane, so the lanes read the chunks in the order in which LDS holds them
+  __device__ __forceinline__ void load_direct(const Args& a, int w, int lane, char* kt, char* vt) const {
+    const int c = lane % kLanes;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int in_tile = w * (ROWS / NW) + row_in_wave(i, lane);
+      const int to = (w * (ROWS / NW) + i * kPass) * kRowB<BF16>;
+      to_lds(static_cast<const uint4*>(a.K) + (at[i] + (c ^ (in_tile & 15))), kt + to);
+      to_lds(static_cast<const uint4*>(a.V) + (at[i] + (BF16 ? c ^ ((in_tile & 7) << 1) : c)), vt + to);
+    }
+  }
+  static __device__ __forceinline__ void to_lds(const uint4* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   }
 
   // 16-byte chunks of the LDS row that a lane's load makes, and where the first of them goes
@@ -210,7 +249,6 @@ struct Block {
   // into LDS; part: some rows of the problem see the block and others do not.  Returns whether elements of V were left
   // out for that.
   __device__ __forceinline__ bool store(char* kt, char* vt, bool part, int w, int lane) const {
-    constexpr uint32_t kAll = ROWS / NW == 32 ? 0xffffffffu : (1u << (ROWS / NW)) - 1u;
     bool left_out = false;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -283,6 +321,12 @@ struct Rows {
           s[n] = dev::mfma_bf16(
               __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kt + k_chunk<true>(32 * n + i, 2 * k + h))),
               __builtin_bit_cast(bf16x8, q[k]), s[n]);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * NS, 0);  // four steps' reads of K ahead of the products
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NS, 0);
+        if (k < 4) __builtin_amdgcn_sched_group_barrier(0x100, NS, 0);
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < 16; ++k)
@@ -296,14 +340,15 @@ struct Rows {
     }
     constexpr uint64_t kAll = NS == 2 ? ~0ull : 0xffffffffull;
     if (!(all_see && there == kAll)) {
+      asm volatile("");  // a branch: taken by few blocks
+      const int up_to = see - p0;
+      const uint64_t mine = (up_to >= 64 ? there : up_to <= 0 ? 0 : there & ((1ull << up_to) - 1)) >> (4 * h);
+      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
 #pragma unroll
       for (int n = 0; n < NS; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int p = 32 * n + dev::mfma_row(e, lane);
-          const bool ok = p0 + p < see && ((there >> p) & 1);
-          s[n][e] = ok ? s[n][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+          s[n][e] = half[n] & (1u << (8 * (e >> 2) + (e & 3))) ? s[n][e] : -INFINITY;
     }
     float top = -INFINITY;
 #pragma unroll
@@ -469,19 +514,36 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   if (threadIdx.x == 0) left_out = 0;
   if (from < end) {
     Block<BF16, PAGE, BN, kWaves> blk;
-    blk.look_up(a.m, p.b, from, end, w, lane);
-    blk.load(a, u.kvh, from, end, w, lane);
-    blk.look_up(a.m, p.b, from + BN, end, w, lane);
     bool cleared = false;
     int buf = 0;
-    for (int p0 = from; p0 < end; p0 += BN, buf ^= 1) {
-      cleared |= blk.store(kt[buf], vt[buf], p0 + BN > least, w, lane);
-      if (lane == 0) there[buf][w] = (uint16_t)blk.there;
-      __syncthreads();
-      if (p0 + BN < end) {
-        blk.load(a, u.kvh, p0 + BN, end, w, lane);
-        blk.look_up(a.m, p.b, p0 + 2 * BN, end, w, lane);
+    // the block at p0 on its way to buffer `to`; 8-bit rows stay in registers until the next round
+    auto fetch = [&](int p0, int to) {
+      blk.find(a, u.kvh, p0, end, w, lane);
+      if constexpr (is8(PAGE)) {
+        blk.load(a, lane);
+      } else {
+        const bool part = p0 + BN > least;
+        if (__builtin_expect(blk.there == blk.kAll && !part, 1)) {
+          blk.load_direct(a, w, lane, kt[to], vt[to]);
+        } else {  // few blocks: the pieces' last, and those on missing pages
+          blk.load(a, lane);
+          cleared |= blk.store(kt[to], vt[to], part, w, lane);
+        }
+        if (lane == 0) there[to][w] = (uint16_t)blk.there;
       }
+      blk.look_up(a.m, p.b, p0 + BN, end, w, lane);
+    };
+    blk.look_up(a.m, p.b, from, end, w, lane);
+    fetch(from, 0);
+    for (int p0 = from; p0 < end; p0 += BN, buf ^= 1) {
+      if constexpr (is8(PAGE)) {
+        cleared |= blk.store(kt[buf], vt[buf], p0 + BN > least, w, lane);
+        if (lane == 0) there[buf][w] = (uint16_t)blk.there;
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wavefront has sent to LDS is there
+      }
+      __syncthreads();
+      if (p0 + BN < end) fetch(p0 + BN, buf ^ 1);
       if (busy && p0 < my_most) {
         uint64_t bits;
         if constexpr (BF16) {
@@ -535,9 +597,10 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   bool cleared = false;
   const int mine = from + w * BN;
   if (mine < end) {
-    Block<BF16, PAGE, BN, 1> blk;
+    Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16> blk;
     blk.look_up(a.m, p.b, mine, end, 0, lane);
-    blk.load(a, u.kvh, mine, end, 0, lane);
+    blk.find(a, u.kvh, mine, end, 0, lane);
+    blk.load(a, lane);
     blk.look_up(a.m, p.b, mine + kWaves * BN, end, 0, lane);
     for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
       __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
@@ -545,7 +608,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
       __builtin_amdgcn_wave_barrier();
       const uint32_t there = blk.there;
       if (p0 + kWaves * BN < end) {
-        blk.load(a, u.kvh, p0 + kWaves * BN, end, 0, lane);
+        blk.find(a, u.kvh, p0 + kWaves * BN, end, 0, lane);
+        blk.load(a, lane);
         blk.look_up(a.m, p.b, p0 + 2 * kWaves * BN, end, 0, lane);
       }
       r.template attend<1>(kt, vt, p0, there, p0 + BN <= least, c, lane);
@@ -690,7 +754,7 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   const Cut c = cut(s);
   const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
                c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.tiles, c.pieces, c.piece,
-               s.scale};
+               (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(kD * page_elem_bytes(s.page_dtype) / 16), s.scale};
   hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {
     e = launch<bf16.value, page.value>(s, c, a, static_cast<hipStream_t>(stream));
