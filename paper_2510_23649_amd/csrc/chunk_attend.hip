@@ -491,9 +491,15 @@ template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
   constexpr int NS = BF16 ? 2 : 1, BN = 32 * NS, M = 128;
   constexpr int kTile = BN * kRowB<BF16>;
-  __shared__ __align__(16) char kt[2][kTile], vt[2][kTile];
-  __shared__ __align__(8) uint16_t there[2][4];
+  // two arrays and two copies of the round, so that the compiler sees that the rows on their way into one buffer are
+  // not those that are read from the other, and does not wait for them there
+  __shared__ __align__(16) char kt0[kTile], vt0[kTile], kt1[kTile], vt1[kTile];
+  __shared__ __align__(8) uint16_t there0[4], there1[4];
   __shared__ int left_out;
+  struct Buffer {
+    char *k, *v;
+    uint16_t* there;
+  };
   const Unit u = unit_of(a, blockIdx.x);
   const Problem p = find_tile<M>(a, u.tile);
   if (p.b < 0) return;
@@ -515,46 +521,49 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   if (from < end) {
     Block<BF16, PAGE, BN, kWaves> blk;
     bool cleared = false;
-    int buf = 0;
     // the block at p0 on its way to buffer `to`; 8-bit rows stay in registers until the next round
-    auto fetch = [&](int p0, int to) {
+    auto fetch = [&](int p0, const Buffer to) __attribute__((always_inline)) {
       blk.find(a, u.kvh, p0, end, w, lane);
       if constexpr (is8(PAGE)) {
         blk.load(a, lane);
       } else {
         const bool part = p0 + BN > least;
         if (__builtin_expect(blk.there == blk.kAll && !part, 1)) {
-          blk.load_direct(a, w, lane, kt[to], vt[to]);
+          blk.load_direct(a, w, lane, to.k, to.v);
         } else {  // few blocks: the pieces' last, and those on missing pages
           blk.load(a, lane);
-          cleared |= blk.store(kt[to], vt[to], part, w, lane);
+          cleared |= blk.store(to.k, to.v, part, w, lane);
         }
-        if (lane == 0) there[to][w] = (uint16_t)blk.there;
+        if (lane == 0) to.there[w] = (uint16_t)blk.there;
       }
       blk.look_up(a.m, p.b, p0 + BN, end, w, lane);
     };
-    blk.look_up(a.m, p.b, from, end, w, lane);
-    fetch(from, 0);
-    for (int p0 = from; p0 < end; p0 += BN, buf ^= 1) {
+    auto round = [&](int p0, const Buffer now, const Buffer next) __attribute__((always_inline)) {
       if constexpr (is8(PAGE)) {
-        cleared |= blk.store(kt[buf], vt[buf], p0 + BN > least, w, lane);
-        if (lane == 0) there[buf][w] = (uint16_t)blk.there;
+        cleared |= blk.store(now.k, now.v, p0 + BN > least, w, lane);
+        if (lane == 0) now.there[w] = (uint16_t)blk.there;
       } else {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wavefront has sent to LDS is there
       }
       __syncthreads();
-      if (p0 + BN < end) fetch(p0 + BN, buf ^ 1);
+      if (p0 + BN < end) fetch(p0 + BN, next);
       if (busy && p0 < my_most) {
         uint64_t bits;
         if constexpr (BF16) {
-          bits = *reinterpret_cast<const uint64_t*>(there[buf]);
+          bits = *reinterpret_cast<const uint64_t*>(now.there);
         } else {
-          bits = there[buf][0] | there[buf][1] << 8 | there[buf][2] << 16 | (uint64_t)there[buf][3] << 24;
+          bits = now.there[0] | now.there[1] << 8 | now.there[2] << 16 | (uint64_t)now.there[3] << 24;
         }
         const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)bits);
         const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(bits >> 32));
-        r.template attend<NS>(kt[buf], vt[buf], p0, (uint64_t)hi << 32 | lo, p0 + BN <= my_least, c, lane);
+        r.template attend<NS>(now.k, now.v, p0, (uint64_t)hi << 32 | lo, p0 + BN <= my_least, c, lane);
       }
+    };
+    blk.look_up(a.m, p.b, from, end, w, lane);
+    fetch(from, Buffer{kt0, vt0, there0});
+    for (int p0 = from; p0 < end; p0 += 2 * BN) {
+      round(p0, Buffer{kt0, vt0, there0}, Buffer{kt1, vt1, there1});
+      if (p0 + BN < end) round(p0 + BN, Buffer{kt1, vt1, there1}, Buffer{kt0, vt0, there0});
     }
     if (cleared) left_out = 1;
   }
