@@ -134,7 +134,8 @@ template <bool BF16>
 __device__ __forceinline__ int k_chunk(int row, int c) {
   return row * kRowB<BF16> + ((c ^ (row & 15)) << 4);
 }
-__device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ ((row & 7) << 1)) << 4); }
+__device__ __forceinline__ int v_turn(int row) { return ((row & 3) << 2) ^ (((row >> 2) & 1) << 1); }
+__device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ v_turn(row)) << 4); }
 
 template <bool BF16, int PAGE, int ROWS, int NW, int LOAD = 16>
 struct Block {
@@ -143,12 +144,18 @@ struct Block {
   static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
   static constexpr int kN = ROWS / NW / kPass;                            // such loads
   static constexpr int kRegs = kLoad / 16;
+  static constexpr int kOut = kRowB<BF16> / 16 / kLanes;                  // 16-byte chunks of LDS that a lane's load makes
   static constexpr uint32_t kAll = ROWS / NW == 32 ? 0xffffffffu : (1u << (ROWS / NW)) - 1u;
-  uint4 k[kN][kRegs], v[kN][kRegs];
-  uint32_t ks[kN], vs[kN];
-  int pg[kN];       // page of each of the lane's rows, one block ahead
-  uint64_t at[kN];  // first 16-byte chunk of each of the lane's rows in the pool; 0 where there is none
-  uint32_t there;   // bit of each of the wavefront's rows
+
+  struct Found {
+    uint32_t at[kN];  // first 16-byte chunk of each of the lane's rows in the pool; 0 where there is none
+    uint32_t there;   // bit of each of the wavefront's rows
+  };
+  struct Held {
+    uint4 x[kN][kRegs];
+    uint32_t scale[kN];
+  };
+  int pg[kN];  // page of each of the lane's rows, one block ahead
 
   static __device__ __forceinline__ int row_in_wave(int i, int lane) { return i * kPass + lane / kLanes; }
 
@@ -163,7 +170,7 @@ struct Block {
   }
 
   // rows of the block at p0, whose pages have been looked up
-  __device__ __forceinline__ void find(const Args& a, int kvh, int p0, int end, int w, int lane) {
+  __device__ __forceinline__ void find(const Args& a, int kvh, int p0, int end, int w, int lane, Found& f) const {
     constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;
     const uint32_t head = ((uint32_t)kvh << a.m.page_log2) * kRow16, in_page = (1u << a.m.page_log2) - 1;
     bool ok[kN], all = true;
@@ -172,58 +179,50 @@ struct Block {
       const uint32_t p = (uint32_t)(p0 + w * (ROWS / NW) + row_in_wave(i, lane));
       ok[i] = ((int)p < end) & ((uint32_t)pg[i] < (uint32_t)a.m.n_pages);
       all &= ok[i];
-      const uint64_t x = (uint64_t)(uint32_t)pg[i] * a.page16 + (head + (p & in_page) * kRow16);
-      at[i] = ok[i] ? x : 0;
+      const uint32_t x = (uint32_t)pg[i] * a.page16 + (head + (p & in_page) * kRow16);
+      f.at[i] = ok[i] ? x : 0;
     }
-    there = kAll;
+    f.there = kAll;
     if (__builtin_expect(__ballot(all) != ~0ull, 0)) {
       asm volatile("");  // a branch: taken by few blocks
-      there = 0;
+      f.there = 0;
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const uint64_t v = __ballot(ok[i]);
 #pragma unroll
-        for (int j = 0; j < kPass; ++j) there |= (uint32_t)((v >> (j * kLanes)) & 1) << (i * kPass + j);
+        for (int j = 0; j < kPass; ++j) f.there |= (uint32_t)((v >> (j * kLanes)) & 1) << (i * kPass + j);
       }
     }
   }
 
-  // the rows found, into registers; what is not there reads row 0
-  __device__ __forceinline__ void load(const Args& a, int lane) {
+  // the rows found, of K or of V, into registers; what is not there reads row 0
+  static __device__ __forceinline__ void load(const void* base, const uint8_t* scale, const Found& f, int lane, Held& r) {
     const int c = lane % kLanes;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
 #pragma unroll
-      for (int j = 0; j < kRegs; ++j) {
-        k[i][j] = static_cast<const uint4*>(a.K)[at[i] + c * kRegs + j];
-        v[i][j] = static_cast<const uint4*>(a.V)[at[i] + c * kRegs + j];
-      }
-      if constexpr (is8(PAGE)) {  // 16 codes: half a scale block; a row has 8 chunks and 4 scales
-        ks[i] = a.K_scale[(at[i] + c) >> 1];
-        vs[i] = a.V_scale[(at[i] + c) >> 1];
-      }
+      for (int j = 0; j < kRegs; ++j) r.x[i][j] = static_cast<const uint4*>(base)[(size_t)(f.at[i] + c * kRegs + j)];
+      // 16 codes are half a scale block; a row has 8 chunks and 4 scales
+      if constexpr (is8(PAGE)) r.scale[i] = scale[(f.at[i] + c) >> 1];
     }
   }
 
-  // the rows found, all of them there and of the type that LDS holds, straight into LDS: a wavefront's load fills 1 KB,
-  // 16 bytes a lane, so the lanes read the chunks in the order in which LDS holds them
-  __device__ __forceinline__ void load_direct(const Args& a, int w, int lane, char* kt, char* vt) const {
+  // The rows found, of the type that LDS holds, straight into LDS: a wavefront's load fills 1 KB, 16 bytes a lane, so the
+  // lanes read the chunks in the order in which LDS holds them.
+  template <bool V>
+  static __device__ __forceinline__ void load_direct(const void* base, const Found& f, int w, int lane, char* to) {
     const int c = lane % kLanes;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int in_tile = w * (ROWS / NW) + row_in_wave(i, lane);
-      const int to = (w * (ROWS / NW) + i * kPass) * kRowB<BF16>;
-      to_lds(static_cast<const uint4*>(a.K) + (at[i] + (c ^ (in_tile & 15))), kt + to);
-      to_lds(static_cast<const uint4*>(a.V) + (at[i] + (BF16 ? c ^ ((in_tile & 7) << 1) : c)), vt + to);
+      const int row = w * (ROWS / NW) + row_in_wave(i, lane);
+      const int turned = V ? (BF16 ? c ^ v_turn(row) : c) : c ^ (row & 15);
+      const uint4* from = static_cast<const uint4*>(base) + (size_t)(f.at[i] + turned);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)from,
+          (__attribute__((address_space(3))) void*)(to + (w * (ROWS / NW) + i * kPass) * kRowB<BF16>), 16, 0, 0);
     }
   }
-  static __device__ __forceinline__ void to_lds(const uint4* from, char* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-  }
 
-  // 16-byte chunks of the LDS row that a lane's load makes, and where the first of them goes
-  static constexpr int kOut = kRowB<BF16> / 16 / kLanes;
   static __device__ __forceinline__ void widen(const uint4 (&x)[kRegs], uint32_t byte, uint4 (&o)[kOut]) {
     if constexpr (!is8(PAGE)) {
 #pragma unroll
@@ -246,32 +245,40 @@ struct Block {
     }
   }
 
-  // into LDS; part: some rows of the problem see the block and others do not.  Returns whether elements of V were left
-  // out for that.
-  __device__ __forceinline__ bool store(char* kt, char* vt, bool part, int w, int lane) const {
+  static __device__ __forceinline__ void store_k(const Held& r, int w, int lane, char* kt) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int row = w * (ROWS / NW) + row_in_wave(i, lane), c = (lane % kLanes) * kOut;
+      uint4 o[kOut];
+      widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
+#pragma unroll
+      for (int j = 0; j < kOut; ++j) *reinterpret_cast<uint4*>(kt + k_chunk<BF16>(row, c + j)) = o[j];
+    }
+  }
+
+  // V rows that are not there become zeros.  part: some rows of the problem see the block and others do not.  Returns
+  // whether elements were left out for that.
+  static __device__ __forceinline__ bool store_v(const Held& r, uint32_t there, bool part, int w, int lane, char* vt) {
     bool left_out = false;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int in_wave = row_in_wave(i, lane), row = w * (ROWS / NW) + in_wave, c = (lane % kLanes) * kOut;
-      uint4 ko[kOut], vo[kOut];
-      widen(k[i], is8(PAGE) ? ks[i] : 0u, ko);
-      widen(v[i], is8(PAGE) ? vs[i] : 0u, vo);
+      uint4 o[kOut];
+      widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
       if (there != kAll && !((there >> in_wave) & 1)) {
 #pragma unroll
-        for (int j = 0; j < kOut; ++j) vo[j] = make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < kOut; ++j) o[j] = make_uint4(0, 0, 0, 0);
       }
       if (part) {
 #pragma unroll
         for (int j = 0; j < kOut; ++j) {
-          left_out |= odd<BF16>(vo[j].x) || odd<BF16>(vo[j].y) || odd<BF16>(vo[j].z) || odd<BF16>(vo[j].w);
-          vo[j] = make_uint4(clear<BF16>(vo[j].x), clear<BF16>(vo[j].y), clear<BF16>(vo[j].z), clear<BF16>(vo[j].w));
+          left_out |= odd<BF16>(o[j].x) || odd<BF16>(o[j].y) || odd<BF16>(o[j].z) || odd<BF16>(o[j].w);
+          o[j] = make_uint4(clear<BF16>(o[j].x), clear<BF16>(o[j].y), clear<BF16>(o[j].z), clear<BF16>(o[j].w));
         }
       }
 #pragma unroll
-      for (int j = 0; j < kOut; ++j) {
-        *reinterpret_cast<uint4*>(kt + k_chunk<BF16>(row, c + j)) = ko[j];
-        *reinterpret_cast<uint4*>(vt + (BF16 ? v_chunk(row, c + j) : row * kRowB<false> + ((c + j) << 4))) = vo[j];
-      }
+      for (int j = 0; j < kOut; ++j)
+        *reinterpret_cast<uint4*>(vt + (BF16 ? v_chunk(row, c + j) : row * kRowB<false> + ((c + j) << 4))) = o[j];
     }
     return left_out;
   }
@@ -303,115 +310,176 @@ struct Rows {
     sum = 0.0f;
   }
 
-  // NS blocks of 32 positions from p0 in LDS, rows `there`; c: scale in log2
-  template <int NS>
-  __device__ __forceinline__ void attend(const char* kt, const char* vt, int p0, uint64_t there, bool all_see,
-                                         float c, int lane) {
-    const int h = lane >> 5, i = lane & 31;
-    f32x16 s[NS];
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
+  __device__ __forceinline__ f32x16 scores_step(const char* kt, int k, f32x16 s, int lane) const {
+    const int i = lane & 31, h = lane >> 5;
     if constexpr (BF16) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-          s[n] = dev::mfma_bf16(
-              __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kt + k_chunk<true>(32 * n + i, 2 * k + h))),
-              __builtin_bit_cast(bf16x8, q[k]), s[n]);
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * NS, 0);  // four steps' reads of K ahead of the products
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, NS, 0);
-        if (k < 4) __builtin_amdgcn_sched_group_barrier(0x100, NS, 0);
-      }
+      return dev::mfma_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kt + k_chunk<true>(i, 2 * k + h))),
+                            __builtin_bit_cast(bf16x8, q[k]), s);
     } else {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(kt + k_chunk<false>(i, 2 * k + h));
+      const f32x4 y = __builtin_bit_cast(f32x4, q[k]);
 #pragma unroll
-      for (int k = 0; k < 16; ++k)
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(kt + k_chunk<false>(32 * n + i, 2 * k + h));
-          const f32x4 y = __builtin_bit_cast(f32x4, q[k]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], s[n], 0, 0, 0);
-        }
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], s, 0, 0, 0);
+      return s;
     }
-    constexpr uint64_t kAll = NS == 2 ? ~0ull : 0xffffffffull;
-    if (!(all_see && there == kAll)) {
-      asm volatile("");  // a branch: taken by few blocks
-      const int up_to = see - p0;
-      const uint64_t mine = (up_to >= 64 ? there : up_to <= 0 ? 0 : there & ((1ull << up_to) - 1)) >> (4 * h);
-      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+  }
+  // scores of 32 positions in LDS
+  __device__ __forceinline__ f32x16 scores(const char* kt, int lane) const {
+    f32x16 s = zeros();
 #pragma unroll
-      for (int n = 0; n < NS; ++n)
+    for (int k = 0; k < (BF16 ? 8 : 16); ++k) s = scores_step(kt, k, s, lane);
+    return s;
+  }
+  static __device__ __forceinline__ f32x16 zeros() {
+    f32x16 z;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[n][e] = half[n] & (1u << (8 * (e >> 2) + (e & 3))) ? s[n][e] : -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+    return z;
+  }
+
+  // scores of the 32 positions from p0 that the row does not see, or that are not there, become -infinity
+  __device__ __forceinline__ void mask(f32x16& s, int p0, uint32_t there, int lane) const {
+    const int up_to = see - p0;
+    const uint32_t mine = (up_to >= 32 ? there : up_to <= 0 ? 0u : there & ((1u << up_to) - 1)) >> (4 * (lane >> 5));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? s[e] : -INFINITY;
+  }
+
+  static __device__ __forceinline__ float largest(const f32x16& s) {
     float top = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
-    top = max_halves(top) * c;
-    if (__any(top > mx + kLag)) {
-      const float to = fmaxf(mx, top);
-      const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mx - to);
-      sum *= f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[t][e] *= f;
-      mx = to;
-    }
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+    return top;
+  }
+
+  // weights of 32 positions at the running maximum, and their sum
+  __device__ __forceinline__ float weigh(const f32x16& s, float c, f32x16& w) const {
     const float base = mx == -INFINITY ? 0.0f : mx;
     float add = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
+    for (int e = 0; e < 16; ++e) {
+      w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base));
+      add += w[e];
+    }
+    return add;
+  }
+  // the running maximum up to `top`
+  __device__ __forceinline__ void raise(float top) {
+    const float to = fmaxf(mx, top);
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mx - to);
+    sum *= f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -base));
-        add += s[n][e];
-      }
-    sum += add;
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] *= f;
+    mx = to;
+  }
+
+  struct Weights {  // of 32 positions as the second product's operand
+    uint4 half[2];
+  };
+  static __device__ __forceinline__ Weights pack(const f32x16& w) {
+    Weights x;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      x.half[k] = make_uint4(dev::pack_bf16(w[8 * k], w[8 * k + 1]), dev::pack_bf16(w[8 * k + 2], w[8 * k + 3]),
+                             dev::pack_bf16(w[8 * k + 4], w[8 * k + 5]), dev::pack_bf16(w[8 * k + 6], w[8 * k + 7]));
+    return x;
+  }
+  // O += weights of 16 positions (half k of 32) times 32 elements (t) of their V rows
+  __device__ __forceinline__ void output_step(const char* vt, const Weights& x, int k, int t, int lane) {
+    // a transposing read: the 16 lanes of a group point at 4 rows of 16 elements, lane g gets column g
+    const int g = lane & 15, h = lane >> 5;
+    s16x4 v[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = 16 * k + 8 * j + 4 * h + (g >> 2);
+      const int chunk = 4 * t + 2 * ((lane >> 4) & 1) + ((g & 3) >> 1);
+      v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4*)(vt + v_chunk(row, chunk) + 8 * (g & 1)));
+    }
+    o[t] = dev::mfma_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)),
+                          __builtin_bit_cast(bf16x8, x.half[k]), o[t]);
+  }
+  __device__ __forceinline__ void output(const char* vt, const Weights& x, int lane) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) output_step(vt, x, k, t, lane);
+  }
+
+  // the weights of s, at a maximum that is raised where it has to be
+  __device__ __forceinline__ f32x16 settle(const f32x16& s, float c) {
+    f32x16 w;
+    const float top = max_halves(largest(s)) * c;
+    if (__any(top > mx + kLag)) raise(top);  // (-inf > -inf is false: nothing seen so far, nothing to do)
+    sum += weigh(s, c, w);
+    return w;
+  }
+
+  // 32 positions from p0 in LDS, rows `there`; c: scale in log2
+  __device__ __forceinline__ void attend(const char* kt, const char* vt, int p0, uint32_t there, bool all_see, float c,
+                                         int lane) {
+    f32x16 s = scores(kt, lane);
+    if (!(all_see && there == 0xffffffffu)) {
+      asm volatile("");  // a branch: taken by few blocks
+      mask(s, p0, there, lane);
+    }
+    const f32x16 w = settle(s, c);
     if constexpr (BF16) {
-      const int g = lane & 15;
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint4 pw = make_uint4(dev::pack_bf16(s[n][8 * k], s[n][8 * k + 1]),
-                                      dev::pack_bf16(s[n][8 * k + 2], s[n][8 * k + 3]),
-                                      dev::pack_bf16(s[n][8 * k + 4], s[n][8 * k + 5]),
-                                      dev::pack_bf16(s[n][8 * k + 6], s[n][8 * k + 7]));
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            // a transposing read: the 16 lanes of a group point at 4 rows of 16 elements, lane g gets column g
-            s16x4 x[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int row = 32 * n + 16 * k + 8 * j + 4 * h + (g >> 2);
-              const int chunk = 4 * t + 2 * ((lane >> 4) & 1) + ((g & 3) >> 1);
-              x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) s16x4*)(vt + v_chunk(row, chunk) + 8 * (g & 1)));
-            }
-            const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-            o[t] = dev::mfma_bf16(v, __builtin_bit_cast(bf16x8, pw), o[t]);
-          }
-        }
+      output(vt, pack(w), lane);
     } else {
 #pragma unroll
-      for (int n = 0; n < NS; ++n)
+      for (int e = 0; e < 16; ++e) {
+        const float* row = reinterpret_cast<const float*>(vt + dev::mfma_row(e, lane) * kRowB<false>);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float* row = reinterpret_cast<const float*>(vt + (32 * n + dev::mfma_row(e, lane)) * kRowB<false>);
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[32 * t + i], s[n][e], o[t], 0, 0, 0);
-        }
+        for (int t = 0; t < 4; ++t)
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[32 * t + (lane & 31)], w[e], o[t], 0, 0, 0);
+      }
     }
+  }
+
+  // One step of the pipeline: the weights of the scores s, between the products of the 32 positions after them (scores
+  // into `next`, from kt) and of those before them (weights x, V rows from vt).  The weights are made at the maximum so
+  // far, and again in the rare case that it has to be raised; x then becomes those of s.
+  template <bool BEFORE>
+  __device__ __forceinline__ void step(const f32x16& s, f32x16& next, Weights& x, const char* kt, const char* vt, float c,
+                                       int lane) {
+    f32x16 w;
+    next = zeros();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      next = scores_step(kt, k, next, lane);
+      if (BEFORE) output_step(vt, x, k >> 2, k & 3, lane);
+    }
+    float add = weigh(s, c, w);
+    const float top = max_halves(largest(s)) * c;
+    x = pack(w);
+    // made here, between the products, and not only once the maximum is known to stand
+    asm volatile("" : "+v"(x.half[0].x), "+v"(x.half[0].y), "+v"(x.half[0].z), "+v"(x.half[0].w), "+v"(x.half[1].x),
+                      "+v"(x.half[1].y), "+v"(x.half[1].z), "+v"(x.half[1].w), "+v"(add));
+#if 1
+    __builtin_amdgcn_sched_group_barrier(0x100, BEFORE ? 6 : 4, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, BEFORE ? 2 : 1, 0);
+      if (BEFORE) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+#endif
+    if (__any(top > mx + kLag)) {
+      raise(top);
+      add = weigh(s, c, w);
+      x = pack(w);
+    }
+    sum += add;
   }
 };
 
@@ -487,19 +555,190 @@ __device__ __forceinline__ Unit unit_of(const Args& a, int i) {
   return u;
 }
 
+// The four wavefronts' bits of a block's rows, as scalars.
+template <int BITS>
+__device__ __forceinline__ uint64_t gather_there(const uint16_t* there) {
+  uint64_t x;
+  if constexpr (BITS == 16) x = *reinterpret_cast<const uint64_t*>(there);
+  else x = there[0] | there[1] << 8 | there[2] << 16 | (uint64_t)there[3] << 24;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (uint64_t)hi << 32 | lo;
+}
+
+// The rounds of a tile in bf16: blocks of 64 positions, two steps (Rows::step) a round.  Round t multiplies with V of
+// block t and with K of block t + 1 while K of block t + 2 and V of block t + 1 are on their way.  Even rounds read K from
+// buffer 1 and V from buffer 0, odd ones the others: arrays and code of their own, so that the compiler sees that the
+// rows on their way are not those that are read, and does not wait for them.
+template <int PAGE>
+struct TileLoop {
+  static constexpr int BN = 64;
+  using B = Block<true, PAGE, BN, kWaves>;
+  const Args& a;
+  const Problem& p;
+  int kvh, w, lane, from, end, least, my_least;
+  bool busy, cleared;
+  float c;
+  Rows<true>& r;
+  uint16_t (*there)[4];  // of four blocks
+  B blk;
+  typename B::Found fk, fv;  // block t + 2's rows, block t + 1's
+  typename B::Held hk, hv;
+  f32x16 s;
+  typename Rows<true>::Weights x;
+
+  // block i's rows on their way: of K
+  __device__ __forceinline__ void fetch_k(int i, char* kt) {
+    blk.find(a, kvh, from + i * BN, end, w, lane, fk);
+    if constexpr (is8(PAGE)) B::load(a.K, a.K_scale, fk, lane, hk);
+    else B::template load_direct<false>(a.K, fk, w, lane, kt);
+    if (lane == 0) there[i & 3][w] = (uint16_t)fk.there;
+    blk.look_up(a.m, p.b, from + (i + 1) * BN, end, w, lane);
+  }
+  // of V, found before
+  __device__ __forceinline__ void fetch_v(int i, char* vt) {
+    if constexpr (is8(PAGE)) {
+      B::load(a.V, a.V_scale, fv, lane, hv);
+    } else {
+      const bool part = from + (i + 1) * BN > least;
+      if (__builtin_expect(fv.there == B::kAll && !part, 1)) {
+        B::template load_direct<true>(a.V, fv, w, lane, vt);
+      } else {  // few blocks: the pieces' last, and those on missing pages
+        B::load(a.V, nullptr, fv, lane, hv);
+        cleared |= B::store_v(hv, fv.there, part, w, lane, vt);
+      }
+    }
+  }
+  // what came through registers goes into LDS; all that this wavefront has fetched is there
+  __device__ __forceinline__ void arrive(bool k, char* kt, int i_v, char* vt) {
+    if constexpr (is8(PAGE)) {
+      if (k) B::store_k(hk, w, lane, kt);
+      cleared |= B::store_v(hv, fv.there, from + (i_v + 1) * BN > least, w, lane, vt);
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void mask_scores(f32x16& y, int p0, uint32_t bits) {
+    if (__builtin_expect(!(p0 + 32 <= my_least && bits == 0xffffffffu), 0)) {
+      asm volatile("");  // a branch: taken by few blocks
+      r.mask(y, p0, bits, lane);
+    }
+  }
+
+  // round t of n - 1; kt, vt: what it reads; kt_to, vt_to: where the rows of blocks t + 2 and t + 1 go
+  __device__ __forceinline__ void round(int t, int n, char* kt, char* vt, char* kt_to, char* vt_to) {
+    arrive(true, kt, t, vt);
+    __syncthreads();
+    fv = fk;  // (block t + 1's rows)
+    if (t + 2 < n) fetch_k(t + 2, kt_to);
+    fetch_v(t + 1, vt_to);
+    if (!busy) return;
+    const int p0 = from + t * BN;
+    f32x16 next;
+    mask_scores(s, p0 + 32, (uint32_t)(gather_there<16>(there[t & 3]) >> 32));
+    r.template step<true>(s, next, x, kt, vt, c, lane);
+    mask_scores(next, p0 + BN, (uint32_t)gather_there<16>(there[(t + 1) & 3]));
+    r.template step<true>(next, s, x, kt + 32 * kRowB<true>, vt + 32 * kRowB<true>, c, lane);
+  }
+
+  __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
+    const int n = (end - from + BN - 1) / BN;
+    blk.look_up(a.m, p.b, from, end, w, lane);
+    fetch_k(0, kt0);
+    if constexpr (is8(PAGE)) B::store_k(hk, w, lane, kt0);
+    fv = fk;
+    if (n > 1) fetch_k(1, kt1);
+    fetch_v(0, vt0);
+    if constexpr (!is8(PAGE)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (busy) {
+      f32x16 first = r.scores(kt0, lane);
+      mask_scores(first, from, (uint32_t)gather_there<16>(there[0]));
+      r.template step<false>(first, s, x, kt0 + 32 * kRowB<true>, nullptr, c, lane);
+    }
+    int t = 0;
+    for (; t + 2 < n; t += 2) {
+      round(t, n, kt1, vt0, kt0, vt1);
+      round(t + 1, n, kt0, vt1, kt1, vt0);
+    }
+    if (t + 1 < n) {
+      round(t, n, kt1, vt0, kt0, vt1);
+      ++t;
+    }
+    char* const vt = t & 1 ? vt1 : vt0;
+    arrive(false, nullptr, t, vt);
+    __syncthreads();
+    if (busy) {
+      mask_scores(s, from + t * BN + 32, (uint32_t)(gather_there<16>(there[t & 3]) >> 32));
+      r.output(vt, x, lane);
+      x = Rows<true>::pack(r.settle(s, c));
+      r.output(vt + 32 * kRowB<true>, x, lane);
+    }
+  }
+};
+
+// The rounds of a tile in fp32: blocks of 32 positions, the next one on its way.
+template <int PAGE>
+struct TileLoopF32 {
+  static constexpr int BN = 32;
+  using B = Block<false, PAGE, BN, kWaves>;
+  const Args& a;
+  const Problem& p;
+  int kvh, w, lane, from, end, least, my_least;
+  bool busy, cleared;
+  float c;
+  Rows<false>& r;
+  uint16_t (*there)[4];
+  B blk;
+  typename B::Found f;
+  typename B::Held hk, hv;
+
+  __device__ __forceinline__ void fetch(int p0, char* kt, char* vt, uint16_t* bits) {
+    blk.find(a, kvh, p0, end, w, lane, f);
+    if constexpr (is8(PAGE)) {
+      B::load(a.K, a.K_scale, f, lane, hk);
+      B::load(a.V, a.V_scale, f, lane, hv);
+    } else {
+      B::template load_direct<false>(a.K, f, w, lane, kt);
+      const bool part = p0 + BN > least;
+      if (__builtin_expect(f.there == B::kAll && !part, 1)) {
+        B::template load_direct<true>(a.V, f, w, lane, vt);
+      } else {
+        B::load(a.V, nullptr, f, lane, hv);
+        cleared |= B::store_v(hv, f.there, part, w, lane, vt);
+      }
+    }
+    if (lane == 0) bits[w] = (uint16_t)f.there;
+    blk.look_up(a.m, p.b, p0 + BN, end, w, lane);
+  }
+  __device__ __forceinline__ void round(int p0, char* kt, char* vt, const uint16_t* bits, char* kt_to, char* vt_to,
+                                        uint16_t* bits_to) {
+    if constexpr (is8(PAGE)) {
+      B::store_k(hk, w, lane, kt);
+      cleared |= B::store_v(hv, f.there, p0 + BN > least, w, lane, vt);
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __syncthreads();
+    if (p0 + BN < end) fetch(p0 + BN, kt_to, vt_to, bits_to);
+    if (busy) r.attend(kt, vt, p0, (uint32_t)gather_there<8>(bits), p0 + BN <= my_least, c, lane);
+  }
+  __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
+    blk.look_up(a.m, p.b, from, end, w, lane);
+    fetch(from, kt0, vt0, there[0]);
+    for (int p0 = from; p0 < end; p0 += 2 * BN) {
+      round(p0, kt0, vt0, there[0], kt1, vt1, there[1]);
+      if (p0 + BN < end) round(p0 + BN, kt1, vt1, there[1], kt0, vt0, there[0]);
+    }
+  }
+};
+
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
-  constexpr int NS = BF16 ? 2 : 1, BN = 32 * NS, M = 128;
-  constexpr int kTile = BN * kRowB<BF16>;
-  // two arrays and two copies of the round, so that the compiler sees that the rows on their way into one buffer are
-  // not those that are read from the other, and does not wait for them there
+  using Loop = std::conditional_t<BF16, TileLoop<PAGE>, TileLoopF32<PAGE>>;
+  constexpr int M = 128, BN = Loop::BN, kTile = BN * kRowB<BF16>;
   __shared__ __align__(16) char kt0[kTile], vt0[kTile], kt1[kTile], vt1[kTile];
-  __shared__ __align__(8) uint16_t there0[4], there1[4];
+  __shared__ __align__(8) uint16_t there[4][4];
   __shared__ int left_out;
-  struct Buffer {
-    char *k, *v;
-    uint16_t* there;
-  };
   const Unit u = unit_of(a, blockIdx.x);
   const Problem p = find_tile<M>(a, u.tile);
   if (p.b < 0) return;
@@ -508,64 +747,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
   const int from = u.piece * a.piece, end = min(most, from + a.piece);
   if (from >= end && u.piece > 0) return;  // (piece 0 writes the rows that see nothing)
-  const int mine = p.r0 + w * 32 + (lane & 31);  // rows behind the last repeat it
+  const int mine = p.r0 + w * 32 + (lane & 31), last = p.rows - 1;  // rows behind the last repeat it
   Rows<BF16> r;
-  const int real = min(mine, p.rows - 1);
+  const int real = min(mine, last);
   r.see = sees(a, p, real);
   r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
-  const bool busy = p.r0 + w * 32 < p.rows;
-  const int my_least = sees(a, p, min(p.r0 + w * 32, p.rows - 1));
-  const int my_most = sees(a, p, min(p.r0 + w * 32 + 31, p.rows - 1));
-  const float c = log2_scale(a);
   if (threadIdx.x == 0) left_out = 0;
   if (from < end) {
-    Block<BF16, PAGE, BN, kWaves> blk;
-    bool cleared = false;
-    // the block at p0 on its way to buffer `to`; 8-bit rows stay in registers until the next round
-    auto fetch = [&](int p0, const Buffer to) __attribute__((always_inline)) {
-      blk.find(a, u.kvh, p0, end, w, lane);
-      if constexpr (is8(PAGE)) {
-        blk.load(a, lane);
-      } else {
-        const bool part = p0 + BN > least;
-        if (__builtin_expect(blk.there == blk.kAll && !part, 1)) {
-          blk.load_direct(a, w, lane, to.k, to.v);
-        } else {  // few blocks: the pieces' last, and those on missing pages
-          blk.load(a, lane);
-          cleared |= blk.store(to.k, to.v, part, w, lane);
-        }
-        if (lane == 0) to.there[w] = (uint16_t)blk.there;
-      }
-      blk.look_up(a.m, p.b, p0 + BN, end, w, lane);
-    };
-    auto round = [&](int p0, const Buffer now, const Buffer next) __attribute__((always_inline)) {
-      if constexpr (is8(PAGE)) {
-        cleared |= blk.store(now.k, now.v, p0 + BN > least, w, lane);
-        if (lane == 0) now.there[w] = (uint16_t)blk.there;
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wavefront has sent to LDS is there
-      }
-      __syncthreads();
-      if (p0 + BN < end) fetch(p0 + BN, next);
-      if (busy && p0 < my_most) {
-        uint64_t bits;
-        if constexpr (BF16) {
-          bits = *reinterpret_cast<const uint64_t*>(now.there);
-        } else {
-          bits = now.there[0] | now.there[1] << 8 | now.there[2] << 16 | (uint64_t)now.there[3] << 24;
-        }
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)bits);
-        const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(bits >> 32));
-        r.template attend<NS>(now.k, now.v, p0, (uint64_t)hi << 32 | lo, p0 + BN <= my_least, c, lane);
-      }
-    };
-    blk.look_up(a.m, p.b, from, end, w, lane);
-    fetch(from, Buffer{kt0, vt0, there0});
-    for (int p0 = from; p0 < end; p0 += 2 * BN) {
-      round(p0, Buffer{kt0, vt0, there0}, Buffer{kt1, vt1, there1});
-      if (p0 + BN < end) round(p0 + BN, Buffer{kt1, vt1, there1}, Buffer{kt0, vt0, there0});
-    }
-    if (cleared) left_out = 1;
+    Loop loop{a, p, u.kvh, w, lane, from, end, least, sees(a, p, min(p.r0 + w * 32, last)), p.r0 + w * 32 <= last, false,
+              log2_scale(a), r, there};
+    loop.run(kt0, vt0, kt1, vt1);
+    if (loop.cleared) left_out = 1;
   }
   r.sum = sum_halves(r.sum);
   if (mine < p.rows) {
@@ -606,22 +798,26 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   bool cleared = false;
   const int mine = from + w * BN;
   if (mine < end) {
-    Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16> blk;
+    using B = Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16>;
+    B blk;
+    typename B::Found f;
+    typename B::Held hk, hv;
+    auto fetch = [&](int p0) __attribute__((always_inline)) {
+      blk.find(a, u.kvh, p0, end, 0, lane, f);
+      B::load(a.K, a.K_scale, f, lane, hk);
+      B::load(a.V, a.V_scale, f, lane, hv);
+      blk.look_up(a.m, p.b, p0 + kWaves * BN, end, 0, lane);
+    };
     blk.look_up(a.m, p.b, mine, end, 0, lane);
-    blk.find(a, u.kvh, mine, end, 0, lane);
-    blk.load(a, lane);
-    blk.look_up(a.m, p.b, mine + kWaves * BN, end, 0, lane);
+    fetch(mine);
     for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
       __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
-      cleared |= blk.store(kt, vt, p0 + BN > least, 0, lane);
+      B::store_k(hk, 0, lane, kt);
+      cleared |= B::store_v(hv, f.there, p0 + BN > least, 0, lane, vt);
       __builtin_amdgcn_wave_barrier();
-      const uint32_t there = blk.there;
-      if (p0 + kWaves * BN < end) {
-        blk.find(a, u.kvh, p0 + kWaves * BN, end, 0, lane);
-        blk.load(a, lane);
-        blk.look_up(a.m, p.b, p0 + 2 * kWaves * BN, end, 0, lane);
-      }
-      r.template attend<1>(kt, vt, p0, there, p0 + BN <= least, c, lane);
+      const uint32_t there = f.there;
+      if (p0 + kWaves * BN < end) fetch(p0 + kWaves * BN);
+      r.attend(kt, vt, p0, there, p0 + BN <= least, c, lane);
     }
   }
   // merge the four states: the accumulators, at a common maximum, meet in LDS

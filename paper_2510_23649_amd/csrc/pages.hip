@@ -27,6 +27,9 @@ int check_pages(const lrqk_pages_shape* s) {
   if (s->page < 1 || s->page > 1024 || (s->page & (s->page - 1)) != 0) return LRQK_ESHAPE;
   if (s->max_pages < 1 || (int64_t)s->max_pages * s->page < s->l_max) return LRQK_ESHAPE;
   if (!std::isfinite(s->scale)) return LRQK_ESHAPE;
+  // 16-byte chunks of a pool are counted in 32 bits
+  const int64_t page16 = (int64_t)s->Hkv * s->page * (kD * pages::page_elem_bytes(s->page_dtype) / 16);
+  if (page16 * s->n_pages > (int64_t)1 << 32) return LRQK_ESHAPE;
   return LRQK_OK;
 }
 

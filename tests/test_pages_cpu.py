@@ -24,12 +24,14 @@ def test_shape_limits(lib):
     assert lib.lrqk_validate_pages(good(lib)) == 0
     for kw in (dict(page=1, max_pages=1000), dict(page=1024, max_pages=1), dict(l_cap=1000), dict(l_cap=2000),
                dict(Hq=32, Hkv=4), dict(page_dtype=2), dict(page_dtype=3), dict(kv_dtype=1, page_dtype=1),
-               dict(kv_dtype=1, page_dtype=2), dict(scale=-1.0), dict(scale=0.0), dict(l_max=1), dict(n_max=100000)):
+               dict(kv_dtype=1, page_dtype=2), dict(scale=-1.0), dict(scale=0.0), dict(l_max=1), dict(n_max=100000),
+               dict(n_pages=1 << 22), dict(n_pages=1 << 23, page_dtype=2)):
         assert lib.lrqk_validate_pages(good(lib, **kw)) == 0, kw
         assert lib.lrqk_pages_workspace_bytes(good(lib, **kw)) > 0, kw
     for kw in (dict(B=0), dict(Hq=30), dict(Hq=36), dict(Hkv=0), dict(d=64), dict(T=0), dict(T=1 << 24), dict(n_max=0),
                dict(l_max=0), dict(l_max=1 << 24), dict(max_pages=62), dict(page=0), dict(page=24), dict(page=2048),
                dict(page=-16), dict(n_pages=0), dict(l_cap=999), dict(l_cap=-1), dict(l_cap=1 << 24), dict(B=3000),
+               dict(n_pages=(1 << 22) + 1), dict(n_pages=(1 << 23) + 1, page_dtype=2), dict(n_pages=(1 << 31) - 1),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(T=(1 << 24) - 1, Hq=256, Hkv=32)):
         assert lib.lrqk_validate_pages(good(lib, **kw)) == -2, kw
         assert lib.lrqk_pages_workspace_bytes(good(lib, **kw)) == 0, kw
