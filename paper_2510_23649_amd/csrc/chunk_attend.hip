@@ -136,74 +136,103 @@ __device__ __forceinline__ int k_chunk(int row, int c) {
 }
 __device__ __forceinline__ int v_turn(int row) { return ((row & 3) << 2) ^ (((row >> 2) & 1) << 1); }
 __device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ v_turn(row)) << 4); }
-
-template <bool BF16, int PAGE, int ROWS, int NW, int LOAD = 16>
+//
+// Blocks and a wavefront's share of them begin at multiples of 16 positions (8 in fp32), so with pages of 16 positions
+// and more up to 16 rows at a time lie one behind the other in one page: their place is one number for the wavefront,
+// and a lane's part of an address does not change from block to block.  SMALL: smaller pages, a table entry for every row.
+template <bool BF16, int PAGE, int ROWS, int NW, int LOAD = 16, bool SMALL = false>
 struct Block {
   static constexpr int kLoad = LOAD;                                      // bytes a lane loads of a row
+  static constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;          // 16-byte chunks of a row in the pool
   static constexpr int kLanes = kD * page_elem_bytes(PAGE) / kLoad;       // lanes a row
   static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
-  static constexpr int kN = ROWS / NW / kPass;                            // such loads
+  static constexpr int kMine = ROWS / NW;                                 // rows of the wavefront
+  static constexpr int kN = kMine / kPass;                                // such loads
   static constexpr int kRegs = kLoad / 16;
   static constexpr int kOut = kRowB<BF16> / 16 / kLanes;                  // 16-byte chunks of LDS that a lane's load makes
-  static constexpr uint32_t kAll = ROWS / NW == 32 ? 0xffffffffu : (1u << (ROWS / NW)) - 1u;
+  static constexpr int kGroup = kMine < 16 ? kMine : 16;                  // rows with one place
+  static constexpr int kGroups = kMine / kGroup;
+  static constexpr uint32_t kAll = kMine == 32 ? 0xffffffffu : (1u << kMine) - 1u;
 
-  struct Found {
-    uint32_t at[kN];  // first 16-byte chunk of each of the lane's rows in the pool; 0 where there is none
-    uint32_t there;   // bit of each of the wavefront's rows
+  struct Found {              // the same in all lanes
+    int p0;                   // position of the wavefront's first row
+    uint32_t place[kGroups];  // chunk of the pool at which a group's first row begins; 0 where there is no page
+    uint32_t there;           // bit of each row
   };
   struct Held {
     uint4 x[kN][kRegs];
     uint32_t scale[kN];
   };
-  int pg[kN];  // page of each of the lane's rows, one block ahead
+  int pg[kGroups];  // the groups' pages, one block ahead
 
   static __device__ __forceinline__ int row_in_wave(int i, int lane) { return i * kPass + lane / kLanes; }
 
-  // table entries for the block at position p0; end: first position that is none
-  __device__ __forceinline__ void look_up(const Map& m, int b, int p0, int end, int w, int lane) {
+  // table entries for the wavefront's rows from position p on; end: first position that is none
+  __device__ __forceinline__ void look_up(const Map& m, int b, int p, int end) {
     const int32_t* table = m.table + (size_t)b * m.max_pages;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int p = p0 + w * (ROWS / NW) + row_in_wave(i, lane);
-      pg[i] = table[(uint32_t)min(p, end - 1) >> m.page_log2];
+    for (int g = 0; g < kGroups; ++g) pg[g] = table[(uint32_t)min(p + g * kGroup, end - 1) >> m.page_log2];
+  }
+
+  // what has been looked up
+  __device__ __forceinline__ void find(const Args& a, int b, int kvh, int p, int end, int lane, Found& f) const {
+    f.p0 = p;
+    f.there = 0;
+    if constexpr (SMALL) {
+      uint32_t at[kN];
+      f.there = find_rows(a, b, kvh, p, end, lane, at);
+      return;
+    }
+    const uint32_t in_page = (1u << a.m.page_log2) - 1;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const uint32_t page = __builtin_amdgcn_readfirstlane(pg[g]);
+      const int q = p + g * kGroup, n = page < (uint32_t)a.m.n_pages ? min(max(end - q, 0), kGroup) : 0;
+      const uint32_t at = page * a.page16 + (((uint32_t)kvh << a.m.page_log2) + ((uint32_t)q & in_page)) * kRow16;
+      f.place[g] = n > 0 ? at : 0;
+      f.there |= ((1u << n) - 1) << (g * kGroup);
     }
   }
 
-  // rows of the block at p0, whose pages have been looked up
-  __device__ __forceinline__ void find(const Args& a, int kvh, int p0, int end, int w, int lane, Found& f) const {
-    constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;
-    const uint32_t head = ((uint32_t)kvh << a.m.page_log2) * kRow16, in_page = (1u << a.m.page_log2) - 1;
-    bool ok[kN], all = true;
+  // Pages of less than 16 positions: the chunk at which each of the lane's rows begins, 0 where there is none; the bits
+  // of the rows that are there.
+  static __device__ __forceinline__ uint32_t find_rows(const Args& a, int b, int kvh, int p, int end, int lane,
+                                                       uint32_t (&at)[kN]) {
+    uint32_t there = 0;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const uint32_t p = (uint32_t)(p0 + w * (ROWS / NW) + row_in_wave(i, lane));
-      ok[i] = ((int)p < end) & ((uint32_t)pg[i] < (uint32_t)a.m.n_pages);
-      all &= ok[i];
-      const uint32_t x = (uint32_t)pg[i] * a.page16 + (head + (p & in_page) * kRow16);
-      f.at[i] = ok[i] ? x : 0;
+      const int q = p + row_in_wave(i, lane);
+      const uint32_t page = a.m.table[(size_t)b * a.m.max_pages + ((uint32_t)min(q, end - 1) >> a.m.page_log2)];
+      const bool ok = (q < end) & (page < (uint32_t)a.m.n_pages);
+      const uint32_t in_page = (uint32_t)q & ((1u << a.m.page_log2) - 1);
+      at[i] = ok ? page * a.page16 + (((uint32_t)kvh << a.m.page_log2) + in_page) * kRow16 : 0;
+      const uint64_t v = __ballot(ok);
+#pragma unroll
+      for (int j = 0; j < kPass; ++j) there |= (uint32_t)((v >> (j * kLanes)) & 1) << (i * kPass + j);
     }
-    f.there = kAll;
-    if (__builtin_expect(__ballot(all) != ~0ull, 0)) {
-      asm volatile("");  // a branch: taken by few blocks
-      f.there = 0;
+    return there;
+  }
+
+  // the rows found, of K or of V, into registers; what is not there reads rows that do not matter
+  static __device__ __forceinline__ void load(const Args& a, int b, int kvh, int end, const void* base,
+                                              const uint8_t* scale, const Found& f, int lane, Held& r) {
+    const int c = lane % kLanes;
+    uint32_t at[kN];
+    if constexpr (SMALL) {
+      find_rows(a, b, kvh, f.p0, end, lane, at);
+    } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        const uint64_t v = __ballot(ok[i]);
-#pragma unroll
-        for (int j = 0; j < kPass; ++j) f.there |= (uint32_t)((v >> (j * kLanes)) & 1) << (i * kPass + j);
+        const int g = i * kPass / kGroup;
+        at[i] = f.place[g] + (uint32_t)(row_in_wave(i, lane) - g * kGroup) * kRow16;
       }
     }
-  }
-
-  // the rows found, of K or of V, into registers; what is not there reads row 0
-  static __device__ __forceinline__ void load(const void* base, const uint8_t* scale, const Found& f, int lane, Held& r) {
-    const int c = lane % kLanes;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
 #pragma unroll
-      for (int j = 0; j < kRegs; ++j) r.x[i][j] = static_cast<const uint4*>(base)[(size_t)(f.at[i] + c * kRegs + j)];
+      for (int j = 0; j < kRegs; ++j) r.x[i][j] = static_cast<const uint4*>(base)[(size_t)(at[i] + c * kRegs + j)];
       // 16 codes are half a scale block; a row has 8 chunks and 4 scales
-      if constexpr (is8(PAGE)) r.scale[i] = scale[(f.at[i] + c) >> 1];
+      if constexpr (is8(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) >> 1)];
     }
   }
 
@@ -211,15 +240,18 @@ struct Block {
   // lanes read the chunks in the order in which LDS holds them.
   template <bool V>
   static __device__ __forceinline__ void load_direct(const void* base, const Found& f, int w, int lane, char* to) {
+    static_assert(kRow16 == kLanes && !SMALL, "one chunk a lane, places for whole groups");
     const int c = lane % kLanes;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int row = w * (ROWS / NW) + row_in_wave(i, lane);
+      const int g = i * kPass / kGroup, row = w * kMine + row_in_wave(i, lane);
       const int turned = V ? (BF16 ? c ^ v_turn(row) : c) : c ^ (row & 15);
-      const uint4* from = static_cast<const uint4*>(base) + (size_t)(f.at[i] + turned);
+      // first what all lanes share, then what a lane adds in every block
+      const char* from = static_cast<const char*>(base) + ((size_t)f.place[g] << 4) +
+                         (uint32_t)(((row_in_wave(i, lane) - g * kGroup) * kRow16 + turned) << 4);
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void*)from,
-          (__attribute__((address_space(3))) void*)(to + (w * (ROWS / NW) + i * kPass) * kRowB<BF16>), 16, 0, 0);
+          (__attribute__((address_space(3))) void*)(to + (w * kMine + i * kPass) * kRowB<BF16>), 16, 0, 0);
     }
   }
 
@@ -248,7 +280,7 @@ struct Block {
   static __device__ __forceinline__ void store_k(const Held& r, int w, int lane, char* kt) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int row = w * (ROWS / NW) + row_in_wave(i, lane), c = (lane % kLanes) * kOut;
+      const int row = w * kMine + row_in_wave(i, lane), c = (lane % kLanes) * kOut;
       uint4 o[kOut];
       widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
 #pragma unroll
@@ -262,7 +294,7 @@ struct Block {
     bool left_out = false;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int in_wave = row_in_wave(i, lane), row = w * (ROWS / NW) + in_wave, c = (lane % kLanes) * kOut;
+      const int in_wave = row_in_wave(i, lane), row = w * kMine + in_wave, c = (lane % kLanes) * kOut;
       uint4 o[kOut];
       widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
       if (there != kAll && !((there >> in_wave) & 1)) {
@@ -588,22 +620,23 @@ struct TileLoop {
 
   // block i's rows on their way: of K
   __device__ __forceinline__ void fetch_k(int i, char* kt) {
-    blk.find(a, kvh, from + i * BN, end, w, lane, fk);
-    if constexpr (is8(PAGE)) B::load(a.K, a.K_scale, fk, lane, hk);
+    const int p0 = from + i * BN + w * B::kMine;
+    blk.find(a, p.b, kvh, p0, end, lane, fk);
+    if constexpr (is8(PAGE)) B::load(a, p.b, kvh, end, a.K, a.K_scale, fk, lane, hk);
     else B::template load_direct<false>(a.K, fk, w, lane, kt);
     if (lane == 0) there[i & 3][w] = (uint16_t)fk.there;
-    blk.look_up(a.m, p.b, from + (i + 1) * BN, end, w, lane);
+    blk.look_up(a.m, p.b, p0 + BN, end);
   }
   // of V, found before
   __device__ __forceinline__ void fetch_v(int i, char* vt) {
     if constexpr (is8(PAGE)) {
-      B::load(a.V, a.V_scale, fv, lane, hv);
+      B::load(a, p.b, kvh, end, a.V, a.V_scale, fv, lane, hv);
     } else {
       const bool part = from + (i + 1) * BN > least;
       if (__builtin_expect(fv.there == B::kAll && !part, 1)) {
         B::template load_direct<true>(a.V, fv, w, lane, vt);
       } else {  // few blocks: the pieces' last, and those on missing pages
-        B::load(a.V, nullptr, fv, lane, hv);
+        B::load(a, p.b, kvh, end, a.V, nullptr, fv, lane, hv);
         cleared |= B::store_v(hv, fv.there, part, w, lane, vt);
       }
     }
@@ -642,7 +675,7 @@ struct TileLoop {
 
   __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
     const int n = (end - from + BN - 1) / BN;
-    blk.look_up(a.m, p.b, from, end, w, lane);
+    blk.look_up(a.m, p.b, from + w * B::kMine, end);
     fetch_k(0, kt0);
     if constexpr (is8(PAGE)) B::store_k(hk, w, lane, kt0);
     fv = fk;
@@ -693,22 +726,23 @@ struct TileLoopF32 {
   typename B::Held hk, hv;
 
   __device__ __forceinline__ void fetch(int p0, char* kt, char* vt, uint16_t* bits) {
-    blk.find(a, kvh, p0, end, w, lane, f);
+    const int mine = p0 + w * B::kMine;
+    blk.find(a, p.b, kvh, mine, end, lane, f);
     if constexpr (is8(PAGE)) {
-      B::load(a.K, a.K_scale, f, lane, hk);
-      B::load(a.V, a.V_scale, f, lane, hv);
+      B::load(a, p.b, kvh, end, a.K, a.K_scale, f, lane, hk);
+      B::load(a, p.b, kvh, end, a.V, a.V_scale, f, lane, hv);
     } else {
       B::template load_direct<false>(a.K, f, w, lane, kt);
       const bool part = p0 + BN > least;
       if (__builtin_expect(f.there == B::kAll && !part, 1)) {
         B::template load_direct<true>(a.V, f, w, lane, vt);
       } else {
-        B::load(a.V, nullptr, f, lane, hv);
+        B::load(a, p.b, kvh, end, a.V, nullptr, f, lane, hv);
         cleared |= B::store_v(hv, f.there, part, w, lane, vt);
       }
     }
     if (lane == 0) bits[w] = (uint16_t)f.there;
-    blk.look_up(a.m, p.b, p0 + BN, end, w, lane);
+    blk.look_up(a.m, p.b, mine + BN, end);
   }
   __device__ __forceinline__ void round(int p0, char* kt, char* vt, const uint16_t* bits, char* kt_to, char* vt_to,
                                         uint16_t* bits_to) {
@@ -723,7 +757,7 @@ struct TileLoopF32 {
     if (busy) r.attend(kt, vt, p0, (uint32_t)gather_there<8>(bits), p0 + BN <= my_least, c, lane);
   }
   __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
-    blk.look_up(a.m, p.b, from, end, w, lane);
+    blk.look_up(a.m, p.b, from + w * B::kMine, end);
     fetch(from, kt0, vt0, there[0]);
     for (int p0 = from; p0 < end; p0 += 2 * BN) {
       round(p0, kt0, vt0, there[0], kt1, vt1, there[1]);
@@ -772,7 +806,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
 }
 
-template <bool BF16, int PAGE>
+template <bool BF16, int PAGE, bool SMALL>
 __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(const Args a) {
   constexpr int M = 32, BN = 32;
   constexpr int kTile = BN * kRowB<BF16>;
@@ -798,17 +832,17 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   bool cleared = false;
   const int mine = from + w * BN;
   if (mine < end) {
-    using B = Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16>;
+    using B = Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16, SMALL>;
     B blk;
     typename B::Found f;
     typename B::Held hk, hv;
     auto fetch = [&](int p0) __attribute__((always_inline)) {
-      blk.find(a, u.kvh, p0, end, 0, lane, f);
-      B::load(a.K, a.K_scale, f, lane, hk);
-      B::load(a.V, a.V_scale, f, lane, hv);
-      blk.look_up(a.m, p.b, p0 + kWaves * BN, end, 0, lane);
+      blk.find(a, p.b, u.kvh, p0, end, lane, f);
+      B::load(a, p.b, u.kvh, end, a.K, a.K_scale, f, lane, hk);
+      B::load(a, p.b, u.kvh, end, a.V, a.V_scale, f, lane, hv);
+      blk.look_up(a.m, p.b, p0 + kWaves * BN, end);
     };
-    blk.look_up(a.m, p.b, mine, end, 0, lane);
+    blk.look_up(a.m, p.b, mine, end);
     fetch(mine);
     for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
       __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
@@ -886,7 +920,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
-// How a call is cut up.  thin: at most 32 rows a sequence and KV head.  The context of a tile is cut into
+// How a call is cut up.  thin: at most 32 rows a sequence and KV head, or pages of less than 16 positions (which the tiles
+// do not read).  The context of a tile is cut into
 // pieces where there are too few tiles to fill 256 compute units with two workgroups each.
 struct Cut {
   bool thin;
@@ -895,7 +930,7 @@ struct Cut {
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
   Cut c;
-  c.thin = (int64_t)s.n_max * G <= 32;
+  c.thin = (int64_t)s.n_max * G <= 32 || s.page < 16;
   const int M = c.thin ? 32 : 128;
   c.tiles = (int)(((int64_t)s.T * G + M - 1) / M) + s.B;  // no fewer than sum_b ceil(n_b G / M)
   const int64_t units = std::max<int64_t>(1, std::max<int64_t>(s.B, ((int64_t)s.T * G + M - 1) / M)) * s.Hkv;
@@ -919,12 +954,11 @@ hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStr
   const dim3 grid((unsigned)((int64_t)c.tiles * s.Hkv * c.pieces));
   if (c.thin) {
     constexpr size_t kLds = (size_t)kWaves * 2 * 32 * kRowB<BF16>;
-    static std::atomic<uint64_t> done{0};
-    if (kLds > 65536 - 2048) {
-      const hipError_t e = raise_dynamic_lds_once(attend_thin_kernel<BF16, PAGE>, kLds, done);
-      if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((attend_thin_kernel<BF16, PAGE>), grid, dim3(kThreads), kLds, st, a);
+    static std::atomic<uint64_t> done{0}, done_small{0};
+    const auto kernel = s.page < 16 ? attend_thin_kernel<BF16, PAGE, true> : attend_thin_kernel<BF16, PAGE, false>;
+    const hipError_t e = raise_dynamic_lds_once(kernel, kLds, s.page < 16 ? done_small : done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLds, st, a);
   } else {
     hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
   }
