@@ -73,19 +73,19 @@ __device__ __forceinline__ Problem find_tile(const Args& a, int tile) {
   p.b = -1;
   int before = 0;
   for (int i0 = 0; i0 < a.m.B; i0 += 64) {
-    const int i = i0 + lane;
-    int tiles = 0;
-    if (i < a.m.B) {
-      const int lo = min(max(a.m.start[i], 0), a.m.T), hi = min(max(a.m.start[i + 1], lo), a.m.T);
-      tiles = ((hi - lo) * a.G + M - 1) / M;
-    }
+    const int i = min(i0 + lane, a.m.B - 1);
+    const int len = a.m.kv_len[i];  // with the starts, not after them
+    const int first = min(max(a.m.start[i], 0), a.m.T), n = min(max(a.m.start[i + 1], first), a.m.T) - first;
+    const int tiles = i0 + lane < a.m.B ? (n * a.G + M - 1) / M : 0;
     const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)tiles);
     const uint64_t past = __ballot(upto > tile);
     if (past) {
       const int j = __builtin_ctzll(past);
       p.b = i0 + j;
       const int mine = __builtin_amdgcn_readlane(upto, j) - __builtin_amdgcn_readlane(tiles, j);
-      p.s = sequence(a.m, p.b);
+      p.s.first = __builtin_amdgcn_readlane(first, j);
+      p.s.n = __builtin_amdgcn_readlane(n, j);
+      p.s.len = max(__builtin_amdgcn_readlane(len, j), 0);
       p.rows = p.s.n * a.G;
       p.r0 = (tile - mine) * M;
       return p;
@@ -264,12 +264,12 @@ struct Block {
       const uint32_t w[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float f[8];
-        decode8<PAGE>(make_uint2(w[2 * j], w[2 * j + 1]), s, f);
+        const uint2 codes = make_uint2(w[2 * j], w[2 * j + 1]);
         if constexpr (BF16) {
-          o[j] = make_uint4(dev::pack_bf16(f[0], f[1]), dev::pack_bf16(f[2], f[3]), dev::pack_bf16(f[4], f[5]),
-                            dev::pack_bf16(f[6], f[7]));
+          o[j] = decode8_bf16<PAGE>(codes, s);
         } else {
+          float f[8];
+          decode8<PAGE>(codes, s, f);
           o[2 * j] = __builtin_bit_cast(uint4, f32x4{f[0], f[1], f[2], f[3]});
           o[2 * j + 1] = __builtin_bit_cast(uint4, f32x4{f[4], f[5], f[6], f[7]});
         }
@@ -514,6 +514,12 @@ struct Rows {
     sum += add;
   }
 };
+
+// What a state (its maximum and sum) counts for at the maximum `top` of several.  One without weights counts for nothing; a
+// NaN's sum stays.
+__device__ __forceinline__ float weight_of(float mx, float sum, float top) {
+  return mx == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(mx - top);
+}
 
 // Four consecutive elements of a row of the output, or of a partial state (the row's max and sum with element 0).
 template <bool BF16>
@@ -806,9 +812,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
 }
 
-template <bool BF16, int PAGE, bool SMALL>
-__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(const Args a) {
-  constexpr int M = 32, BN = 32;
+template <bool BF16, int PAGE, int SETS, bool SMALL>
+__global__ __launch_bounds__(kThreads, BF16 && SETS == 1 ? 2 : 1) void attend_thin_kernel(const Args a) {
+  constexpr int M = 32 * SETS, BN = 32;
   constexpr int kTile = BN * kRowB<BF16>;
   extern __shared__ __align__(16) char lds[];  // per wavefront: K, V
   __shared__ float wm[kWaves][M], ws[kWaves][M];
@@ -821,10 +827,13 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
   const int from = u.piece * a.piece, end = min(most, from + a.piece);
   if (from >= end && u.piece > 0) return;
-  Rows<BF16> r;
-  const int real = min(p.r0 + (lane & 31), p.rows - 1);
-  r.see = sees(a, p, real);
-  r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+  Rows<BF16> r[SETS];
+#pragma unroll
+  for (int j = 0; j < SETS; ++j) {
+    const int real = min(p.r0 + 32 * j + (lane & 31), p.rows - 1);
+    r[j].see = sees(a, p, real);
+    r[j].start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+  }
   const float c = log2_scale(a);
   if (threadIdx.x == 0) left_out = 0;
   char* const kt = lds + w * 2 * kTile;
@@ -851,68 +860,127 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
       __builtin_amdgcn_wave_barrier();
       const uint32_t there = f.there;
       if (p0 + kWaves * BN < end) fetch(p0 + kWaves * BN);
-      r.attend(kt, vt, p0, there, p0 + BN <= least, c, lane);
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) r[j].attend(kt, vt, p0, there, p0 + BN <= least, c, lane);
     }
   }
-  // merge the four states: the accumulators, at a common maximum, meet in LDS
-  r.sum = sum_halves(r.sum);
-  if (lane < M) {
-    wm[w][lane] = r.mx;
-    ws[w][lane] = r.sum;
+  // merge the four states: the accumulators, at a common maximum, meet in LDS, 32 rows at a time
+#pragma unroll
+  for (int j = 0; j < SETS; ++j) {
+    r[j].sum = sum_halves(r[j].sum);
+    if (lane < 32) {
+      wm[w][32 * j + lane] = r[j].mx;
+      ws[w][32 * j + lane] = r[j].sum;
+    }
   }
   __syncthreads();
   if (cleared) left_out = 1;
   const int i = lane & 31, h = lane >> 5;
-  const float top = fmaxf(fmaxf(wm[0][i], wm[1][i]), fmaxf(wm[2][i], wm[3][i]));
-  const float f = r.mx == -INFINITY ? (r.sum == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(r.mx - top);
   float* const acc = reinterpret_cast<float*>(lds);  // [wave][row][128], 16-byte chunks turned by the row
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int j = 0; j < SETS; ++j) {
+    const int r0 = 32 * j;
+    const float top = fmaxf(fmaxf(wm[0][r0 + i], wm[1][r0 + i]), fmaxf(wm[2][r0 + i], wm[3][r0 + i]));
+    const float f = weight_of(r[j].mx, r[j].sum, top);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<f32x4*>(acc + (w * M + i) * kD + 4 * ((8 * t + 2 * e + h) ^ i)) =
-          f32x4{r.o[t][4 * e] * f, r.o[t][4 * e + 1] * f, r.o[t][4 * e + 2] * f, r.o[t][4 * e + 3] * f};
-  __syncthreads();
-  for (int j = threadIdx.x; j < rows * (kD / 4); j += kThreads) {
-    const int row = j / (kD / 4), chunk = j % (kD / 4);
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    float mx = -INFINITY, sum = 0.0f;
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, wm[v][row]);
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(acc + (w * 32 + i) * kD + 4 * ((8 * t + 2 * e + h) ^ i)) =
+            f32x4{r[j].o[t][4 * e] * f, r[j].o[t][4 * e + 1] * f, r[j].o[t][4 * e + 2] * f, r[j].o[t][4 * e + 3] * f};
+    __syncthreads();
+    for (int k = threadIdx.x; k < min(32, rows - r0) * (kD / 4); k += kThreads) {
+      const int row = k / (kD / 4), chunk = k % (kD / 4);
+      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+      float mx = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      const float g = wm[v][row] == -INFINITY ? (ws[v][row] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(wm[v][row] - mx);
-      sum += ws[v][row] * g;
-      x += *reinterpret_cast<const f32x4*>(acc + (v * M + row) * kD + 4 * (chunk ^ row));
+      for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, wm[v][r0 + row]);
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        sum += ws[v][r0 + row] * weight_of(wm[v][r0 + row], ws[v][r0 + row], mx);
+        x += *reinterpret_cast<const f32x4*>(acc + (v * 32 + row) * kD + 4 * (chunk ^ row));
+      }
+      put<BF16>(a, p, u.kvh, p.r0 + r0 + row, u.piece, 4 * chunk, x, mx, sum);
     }
-    put<BF16>(a, p, u.kvh, p.r0 + row, u.piece, 4 * chunk, x, mx, sum);
+    if (j + 1 < SETS) __syncthreads();
   }
   __syncthreads();
   if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
 }
 
-// The pieces of a row's context joined: a wavefront per row, two elements a lane.
-template <bool BF16>
+// The pieces of a row's context joined: W wavefronts a row, each takes its share of the pieces, a piece's maximum and sum
+// in a lane, two elements a lane.  All loads of a share are independent of each other.
+template <bool BF16, int W>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int64_t n_rows) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  __shared__ float part[kWaves][2 + kD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
+  const int64_t at = (int64_t)blockIdx.x * (kWaves / W) + wave / W;
   const int Hq = a.m.Hkv * a.G;
   const int t = (int)min(at / Hq, (int64_t)a.m.T);
   const int b = sequence_of(a.m, t);
-  if (at >= n_rows || b < 0) return;
-  const Seq s = sequence(a.m, b);
-  if (t < s.first || t >= s.first + s.n) return;
-  const int see = min(max(s.len - s.n + (t - s.first) + 1, 0), a.m.l_max);
-  const int pieces = max(1, (see + a.piece - 1) / a.piece);
-  const float* P = a.partials + at * a.pieces * kPartial;
+  bool mine = at < n_rows && b >= 0;
+  int pieces = 0;
+  if (mine) {
+    const Seq s = sequence(a.m, b);
+    mine = t >= s.first && t < s.first + s.n;
+    const int see = min(max(s.len - s.n + (t - s.first) + 1, 0), a.m.l_max);
+    pieces = max(1, (see + a.piece - 1) / a.piece);
+  }
+  if (W == 1 && !mine) return;
   float mx = -INFINITY, sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
-  for (int i = 0; i < pieces; ++i) mx = fmaxf(mx, P[(int64_t)i * kPartial]);
-  for (int i = 0; i < pieces; ++i) {
-    const float* p = P + (int64_t)i * kPartial;
-    const float f = p[0] == -INFINITY ? (p[1] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(p[0] - mx);
-    sum += p[1] * f;
-    x0 += p[4 + 2 * lane] * f;
-    x1 += p[5 + 2 * lane] * f;
+  if (mine) {
+    const float* P = a.partials + at * a.pieces * kPartial;
+    const int share = (pieces + W - 1) / W, lo = min(pieces, w * share), hi = min(pieces, lo + share);
+    for (int i0 = lo; i0 < hi; i0 += 64) {
+      const int n = min(64, hi - i0);
+      const float* p = P + (int64_t)(i0 + min(lane, n - 1)) * kPartial;
+      const float m = lane < n ? p[0] : -INFINITY, l = lane < n ? p[1] : 0.0f;
+      float top = fmaxf(mx, m);
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+      const float f = weight_of(m, l, top), g = weight_of(mx, sum, top);
+      float add = l * f;
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) add += __shfl_xor(add, i);
+      sum = sum * g + add;
+      x0 *= g;
+      x1 *= g;
+      mx = top;
+      p = P + (int64_t)i0 * kPartial + 4 + 2 * lane;
+      for (int i = 0; i < n; i += 4) {
+        float2 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float2*>(p + (int64_t)min(i + j, n - 1) * kPartial);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (i + j < n) {
+            const float k = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i + j));
+            x0 = __builtin_fmaf(k, x[j].x, x0);
+            x1 = __builtin_fmaf(k, x[j].y, x1);
+          }
+      }
+    }
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      part[wave][0] = mx;
+      part[wave][1] = sum;
+    }
+    part[wave][2 + 2 * lane] = x0;
+    part[wave][3 + 2 * lane] = x1;
+    __syncthreads();
+    if (!mine || w != 0) return;
+    float top = mx;
+#pragma unroll
+    for (int i = 1; i < W; ++i) top = fmaxf(top, part[wave + i][0]);
+    sum = x0 = x1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float f = weight_of(part[wave + i][0], part[wave + i][1], top);
+      sum += part[wave + i][1] * f;
+      x0 = __builtin_fmaf(f, part[wave + i][2 + 2 * lane], x0);
+      x1 = __builtin_fmaf(f, part[wave + i][3 + 2 * lane], x1);
+    }
   }
   x0 = sum == 0.0f ? 0.0f : x0 / sum;
   x1 = sum == 0.0f ? 0.0f : x1 / sum;
@@ -920,28 +988,28 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
-// How a call is cut up.  thin: at most 32 rows a sequence and KV head, or pages of less than 16 positions (which the tiles
-// do not read).  The context of a tile is cut into
-// pieces where there are too few tiles to fill 256 compute units with two workgroups each.
+// How a call is cut up.  At most 64 rows a sequence and KV head go the thin way, 32 of them or two sets of 32 in a wavefront;
+// so do pages of less than 16 positions, 32 rows at a time, whatever the number of rows.  The context is cut into pieces
+// until there are `want` workgroups.
 struct Cut {
-  bool thin;
+  int sets;  // thin: 1 or 2; 0: tiles of 128 rows
   int tiles, pieces, piece;
 };
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
+  const int64_t most = (int64_t)s.n_max * G;
   Cut c;
-  c.thin = (int64_t)s.n_max * G <= 32 || s.page < 16;
-  const int M = c.thin ? 32 : 128;
-  c.tiles = (int)(((int64_t)s.T * G + M - 1) / M) + s.B;  // no fewer than sum_b ceil(n_b G / M)
-  const int64_t units = std::max<int64_t>(1, std::max<int64_t>(s.B, ((int64_t)s.T * G + M - 1) / M)) * s.Hkv;
-  const int least = c.thin ? 256 : 1024;
-  const int64_t want = c.thin ? 1024 : 512;
-  int64_t pieces = (want + units - 1) / units;
-  int64_t piece = (s.l_max + pieces - 1) / pieces;
-  piece = std::max<int64_t>(piece, least);
-  piece = (piece + 127) / 128 * 128;
-  c.piece = (int)piece;
-  c.pieces = (int)((s.l_max + piece - 1) / piece);
+  c.sets = most <= 32 || s.page < 16 ? 1 : most <= 64 ? 2 : 0;
+  const int M = c.sets > 0 ? 32 * c.sets : 128;
+  const int tiles = (int)(((int64_t)s.T * G + M - 1) / M);
+  c.tiles = tiles + s.B;  // no fewer than sum_b ceil(n_b G / M)
+  const int64_t units = (int64_t)std::max(s.B, tiles) * s.Hkv;
+  const bool few = most <= 128;
+  const int64_t want = few ? 4096 : 512;
+  const int64_t pieces = (want + units - 1) / units;
+  const int64_t piece = std::max<int64_t>((s.l_max + pieces - 1) / pieces, few ? 256 : 1024);
+  c.piece = (int)((piece + 127) / 128 * 128);
+  c.pieces = (s.l_max + c.piece - 1) / c.piece;
   return c;
 }
 size_t partial_bytes(const lrqk_pages_shape& s) {
@@ -949,23 +1017,33 @@ size_t partial_bytes(const lrqk_pages_shape& s) {
   return c.pieces > 1 ? (size_t)s.T * s.Hq * c.pieces * kPartial * sizeof(float) : 0;
 }
 
+template <bool BF16, int PAGE, int SETS, bool SMALL>
+hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
+  constexpr size_t kLds = (size_t)kWaves * 2 * 32 * kRowB<BF16>;
+  static std::atomic<uint64_t> done{0};
+  const auto kernel = attend_thin_kernel<BF16, PAGE, SETS, SMALL>;
+  const hipError_t e = raise_dynamic_lds_once(kernel, kLds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLds, st, a);
+  return hipSuccess;
+}
+
 template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)c.tiles * s.Hkv * c.pieces));
-  if (c.thin) {
-    constexpr size_t kLds = (size_t)kWaves * 2 * 32 * kRowB<BF16>;
-    static std::atomic<uint64_t> done{0}, done_small{0};
-    const auto kernel = s.page < 16 ? attend_thin_kernel<BF16, PAGE, true> : attend_thin_kernel<BF16, PAGE, false>;
-    const hipError_t e = raise_dynamic_lds_once(kernel, kLds, s.page < 16 ? done_small : done);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLds, st, a);
-  } else {
-    hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
-  }
+  hipError_t e = hipSuccess;
+  if (s.page < 16) e = launch_thin<BF16, PAGE, 1, true>(grid, a, st);
+  else if (c.sets == 1) e = launch_thin<BF16, PAGE, 1, false>(grid, a, st);
+  else if (c.sets == 2) e = launch_thin<BF16, PAGE, 2, false>(grid, a, st);
+  else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
+  if (e != hipSuccess) return e;
   if (a.partials) {
     const int64_t rows = (int64_t)s.T * s.Hq;
-    hipLaunchKernelGGL((attend_join_kernel<BF16>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
-                       a, rows);
+    if (c.pieces > 8)  // a workgroup per row
+      hipLaunchKernelGGL((attend_join_kernel<BF16, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);
+    else
+      hipLaunchKernelGGL((attend_join_kernel<BF16, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0,
+                         st, a, rows);
   }
   return hipGetLastError();
 }

@@ -81,6 +81,25 @@ __device__ __forceinline__ void decode8(uint2 c, float s, float (&x)[8]) {
   }
 }
 
+// The same as four packed bf16 pairs: exact too (a code has at most seven bits, and scales as they are written leave bf16's
+// range of normal numbers by no means).
+template <int PAGE>
+__device__ __forceinline__ uint4 decode8_bf16(uint2 c, float s) {
+  if constexpr (PAGE == LRQK_PAGE_E4M3) {
+    auto pair = [&](uint32_t w, auto high) {
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, high.value));
+    };
+    using std::false_type;
+    using std::true_type;
+    return make_uint4(pair(c.x, false_type{}), pair(c.x, true_type{}), pair(c.y, false_type{}), pair(c.y, true_type{}));
+  } else {
+    float f[8];
+    decode8<PAGE>(c, s, f);
+    return make_uint4(dev::pack_bf16(f[0], f[1]), dev::pack_bf16(f[2], f[3]), dev::pack_bf16(f[4], f[5]),
+                      dev::pack_bf16(f[6], f[7]));
+  }
+}
+
 // The scale byte of a block whose largest magnitude has the bits `top` (compared as integers, so that
 // infinity and NaN win): the smallest e >= kMinExp with max <= 448 2^e or 127 2^e.  448 = 1.75 * 2^8,
 // 127 = 1.984375 * 2^6: one more where the mantissa is above theirs.
