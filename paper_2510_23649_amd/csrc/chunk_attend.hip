@@ -47,7 +47,7 @@ struct Args {
   const void* q;
   void* out;
   float* partials;  // [T*Hq][pieces][kPartial], or null: one piece, straight to out
-  int G, tiles, pieces, piece;
+  int G, units, pieces, piece;  // units: of a KV head, at most
   uint32_t page16;  // 16-byte chunks of a page (of all KV heads)
   float scale;
 };
@@ -61,38 +61,41 @@ using dev::f32x16;
 // Row r of the problem of a sequence: token and query head within the group.
 struct Problem {
   Seq s;
-  int b, r0, rows;  // first row of this workgroup, rows of the sequence
+  int b, piece, r0, rows;  // piece and first row of this workgroup, rows of the sequence
 };
 
-// The sequence and the first row of tile `tile` (M rows each), or b = -1.  Every wavefront finds it for
-// itself, 64 sequences at a time.
+// Unit `unit` of the work of a KV head: a sequence's units are its pieces, last one first, a piece's its tiles (M rows each).  False if there
+// are not that many.  Every wavefront finds it for itself, 64 sequences at a time.
 template <int M>
-__device__ __forceinline__ Problem find_tile(const Args& a, int tile) {
+__device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
   const int lane = threadIdx.x & 63;
-  Problem p;
-  p.b = -1;
   int before = 0;
   for (int i0 = 0; i0 < a.m.B; i0 += 64) {
     const int i = min(i0 + lane, a.m.B - 1);
-    const int len = a.m.kv_len[i];  // with the starts, not after them
+    const int len = max(a.m.kv_len[i], 0);  // with the starts, not after them
     const int first = min(max(a.m.start[i], 0), a.m.T), n = min(max(a.m.start[i + 1], first), a.m.T) - first;
-    const int tiles = i0 + lane < a.m.B ? (n * a.G + M - 1) / M : 0;
-    const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)tiles);
-    const uint64_t past = __ballot(upto > tile);
+    const int tiles = (n * a.G + M - 1) / M, pieces = max(1, (min(len, a.m.l_max) + a.piece - 1) / a.piece);
+    const int units = i0 + lane < a.m.B ? tiles * pieces : 0;
+    const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)units);
+    const uint64_t past = __ballot(upto > unit);
     if (past) {
       const int j = __builtin_ctzll(past);
+      const int mine = unit - (__builtin_amdgcn_readlane(upto, j) - __builtin_amdgcn_readlane(units, j));
+      const int t = __builtin_amdgcn_readlane(tiles, j);
       p.b = i0 + j;
-      const int mine = __builtin_amdgcn_readlane(upto, j) - __builtin_amdgcn_readlane(tiles, j);
       p.s.first = __builtin_amdgcn_readlane(first, j);
       p.s.n = __builtin_amdgcn_readlane(n, j);
-      p.s.len = max(__builtin_amdgcn_readlane(len, j), 0);
+      p.s.len = __builtin_amdgcn_readlane(len, j);
       p.rows = p.s.n * a.G;
-      p.r0 = (tile - mine) * M;
-      return p;
+      // the last tiles of a sequence see most: they come first
+      const int back = __builtin_amdgcn_readlane(units, j) - 1 - mine;
+      p.piece = back / t;
+      p.r0 = (back - p.piece * t) * M;
+      return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
   }
-  return p;
+  return false;
 }
 
 // Positions that a row of the problem sees: [0, result).
@@ -140,15 +143,13 @@ __device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true
 // Blocks and a wavefront's share of them begin at multiples of 16 positions (8 in fp32), so with pages of 16 positions
 // and more up to 16 rows at a time lie one behind the other in one page: their place is one number for the wavefront,
 // and a lane's part of an address does not change from block to block.  SMALL: smaller pages, a table entry for every row.
-template <bool BF16, int PAGE, int ROWS, int NW, int LOAD = 16, bool SMALL = false>
+template <bool BF16, int PAGE, int ROWS, int NW, bool SMALL = false>
 struct Block {
-  static constexpr int kLoad = LOAD;                                      // bytes a lane loads of a row
   static constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;          // 16-byte chunks of a row in the pool
-  static constexpr int kLanes = kD * page_elem_bytes(PAGE) / kLoad;       // lanes a row
+  static constexpr int kLanes = kRow16;                                   // lanes a row: 16 bytes each
   static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
   static constexpr int kMine = ROWS / NW;                                 // rows of the wavefront
   static constexpr int kN = kMine / kPass;                                // such loads
-  static constexpr int kRegs = kLoad / 16;
   static constexpr int kOut = kRowB<BF16> / 16 / kLanes;                  // 16-byte chunks of LDS that a lane's load makes
   static constexpr int kGroup = kMine < 16 ? kMine : 16;                  // rows with one place
   static constexpr int kGroups = kMine / kGroup;
@@ -160,7 +161,7 @@ struct Block {
     uint32_t there;           // bit of each row
   };
   struct Held {
-    uint4 x[kN][kRegs];
+    uint4 x[kN];
     uint32_t scale[kN];
   };
   int pg[kGroups];  // the groups' pages, one block ahead
@@ -229,8 +230,7 @@ struct Block {
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-#pragma unroll
-      for (int j = 0; j < kRegs; ++j) r.x[i][j] = static_cast<const uint4*>(base)[(size_t)(at[i] + c * kRegs + j)];
+      r.x[i] = static_cast<const uint4*>(base)[(size_t)(at[i] + c)];
       // 16 codes are half a scale block; a row has 8 chunks and 4 scales
       if constexpr (is8(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) >> 1)];
     }
@@ -255,13 +255,12 @@ struct Block {
     }
   }
 
-  static __device__ __forceinline__ void widen(const uint4 (&x)[kRegs], uint32_t byte, uint4 (&o)[kOut]) {
+  static __device__ __forceinline__ void widen(const uint4 x, uint32_t byte, uint4 (&o)[kOut]) {
     if constexpr (!is8(PAGE)) {
-#pragma unroll
-      for (int j = 0; j < kOut; ++j) o[j] = x[j];
+      o[0] = x;
     } else {
       const float s = scale_of(byte);
-      const uint32_t w[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint2 codes = make_uint2(w[2 * j], w[2 * j + 1]);
@@ -580,19 +579,6 @@ __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows,
   }
 }
 
-// Workgroups: KV head fastest (its rows stay in one die's L2), then tile, last tiles first: they are the longest.
-struct Unit {
-  int kvh, tile, piece;
-};
-__device__ __forceinline__ Unit unit_of(const Args& a, int i) {
-  Unit u;
-  u.kvh = i % a.m.Hkv;
-  const int j = i / a.m.Hkv;
-  u.tile = a.tiles - 1 - j % a.tiles;
-  u.piece = j / a.tiles;
-  return u;
-}
-
 // The four wavefronts' bits of a block's rows, as scalars.
 template <int BITS>
 __device__ __forceinline__ uint64_t gather_there(const uint16_t* there) {
@@ -778,26 +764,26 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   constexpr int M = 128, BN = Loop::BN, kTile = BN * kRowB<BF16>;
   __shared__ __align__(16) char kt0[kTile], vt0[kTile], kt1[kTile], vt1[kTile];
   __shared__ __align__(8) uint16_t there[4][4];
-  __shared__ int left_out;
-  const Unit u = unit_of(a, blockIdx.x);
-  const Problem p = find_tile<M>(a, u.tile);
-  if (p.b < 0) return;
+  // KV head fastest: the dies take workgroups in turn, so a head's rows stay in one die's L2
+  const int kvh = blockIdx.x % a.m.Hkv;
+  Problem p;
+  if (!find_unit<M>(a, blockIdx.x / a.m.Hkv, p)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = min(M, p.rows - p.r0);
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-  const int from = u.piece * a.piece, end = min(most, from + a.piece);
-  if (from >= end && u.piece > 0) return;  // (piece 0 writes the rows that see nothing)
+  const int from = p.piece * a.piece, end = min(most, from + a.piece);
+  if (from >= end && p.piece > 0) return;  // (piece 0 writes the rows that see nothing)
   const int mine = p.r0 + w * 32 + (lane & 31), last = p.rows - 1;  // rows behind the last repeat it
   Rows<BF16> r;
   const int real = min(mine, last);
   r.see = sees(a, p, real);
-  r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
-  if (threadIdx.x == 0) left_out = 0;
+  r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+  bool cleared = false;
   if (from < end) {
-    Loop loop{a, p, u.kvh, w, lane, from, end, least, sees(a, p, min(p.r0 + w * 32, last)), p.r0 + w * 32 <= last, false,
+    Loop loop{a, p, kvh, w, lane, from, end, least, sees(a, p, min(p.r0 + w * 32, last)), p.r0 + w * 32 <= last, false,
               log2_scale(a), r, there};
     loop.run(kt0, vt0, kt1, vt1);
-    if (loop.cleared) left_out = 1;
+    cleared = loop.cleared;
   }
   r.sum = sum_halves(r.sum);
   if (mine < p.rows) {
@@ -805,11 +791,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        put<BF16>(a, p, u.kvh, mine, u.piece, 32 * t + 8 * e + 4 * (lane >> 5),
+        put<BF16>(a, p, kvh, mine, p.piece, 32 * t + 8 * e + 4 * (lane >> 5),
                   f32x4{r.o[t][4 * e], r.o[t][4 * e + 1], r.o[t][4 * e + 2], r.o[t][4 * e + 3]}, r.mx, r.sum);
   }
-  __syncthreads();
-  if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
+  if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
 }
 
 template <bool BF16, int PAGE, int SETS, bool SMALL>
@@ -818,37 +803,39 @@ __global__ __launch_bounds__(kThreads, BF16 && SETS == 1 ? 2 : 1) void attend_th
   constexpr int kTile = BN * kRowB<BF16>;
   extern __shared__ __align__(16) char lds[];  // per wavefront: K, V
   __shared__ float wm[kWaves][M], ws[kWaves][M];
-  __shared__ int left_out;
-  const Unit u = unit_of(a, blockIdx.x);
-  const Problem p = find_tile<M>(a, u.tile);
-  if (p.b < 0) return;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % a.m.Hkv;
+  // the grid is as large as the chip: how many units there are is known here alone
+  for (int unit = blockIdx.x / a.m.Hkv;; unit += gridDim.x / a.m.Hkv) {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
+  Problem p;
+  if (!find_unit<M>(a, unit, p)) return;
   const int rows = min(M, p.rows - p.r0);
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-  const int from = u.piece * a.piece, end = min(most, from + a.piece);
-  if (from >= end && u.piece > 0) return;
+  const int from = p.piece * a.piece, end = min(most, from + a.piece);
+  if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
   Rows<BF16> r[SETS];
 #pragma unroll
   for (int j = 0; j < SETS; ++j) {
     const int real = min(p.r0 + 32 * j + (lane & 31), p.rows - 1);
     r[j].see = sees(a, p, real);
-    r[j].start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + u.kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    r[j].start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
   }
   const float c = log2_scale(a);
-  if (threadIdx.x == 0) left_out = 0;
   char* const kt = lds + w * 2 * kTile;
   char* const vt = kt + kTile;
   bool cleared = false;
   const int mine = from + w * BN;
   if (mine < end) {
-    using B = Block<BF16, PAGE, BN, 1, PAGE == LRQK_PAGE_F32 ? 32 : 16, SMALL>;
+    using B = Block<BF16, PAGE, BN, 1, SMALL>;
     B blk;
     typename B::Found f;
     typename B::Held hk, hv;
     auto fetch = [&](int p0) __attribute__((always_inline)) {
-      blk.find(a, p.b, u.kvh, p0, end, lane, f);
-      B::load(a, p.b, u.kvh, end, a.K, a.K_scale, f, lane, hk);
-      B::load(a, p.b, u.kvh, end, a.V, a.V_scale, f, lane, hv);
+      blk.find(a, p.b, kvh, p0, end, lane, f);
+      B::load(a, p.b, kvh, end, a.K, a.K_scale, f, lane, hk);
+      B::load(a, p.b, kvh, end, a.V, a.V_scale, f, lane, hv);
       blk.look_up(a.m, p.b, p0 + kWaves * BN, end);
     };
     blk.look_up(a.m, p.b, mine, end);
@@ -874,7 +861,6 @@ __global__ __launch_bounds__(kThreads, BF16 && SETS == 1 ? 2 : 1) void attend_th
     }
   }
   __syncthreads();
-  if (cleared) left_out = 1;
   const int i = lane & 31, h = lane >> 5;
   float* const acc = reinterpret_cast<float*>(lds);  // [wave][row][128], 16-byte chunks turned by the row
 #pragma unroll
@@ -900,12 +886,12 @@ __global__ __launch_bounds__(kThreads, BF16 && SETS == 1 ? 2 : 1) void attend_th
         sum += ws[v][r0 + row] * weight_of(wm[v][r0 + row], ws[v][r0 + row], mx);
         x += *reinterpret_cast<const f32x4*>(acc + (v * 32 + row) * kD + 4 * (chunk ^ row));
       }
-      put<BF16>(a, p, u.kvh, p.r0 + r0 + row, u.piece, 4 * chunk, x, mx, sum);
+      put<BF16>(a, p, kvh, p.r0 + r0 + row, p.piece, 4 * chunk, x, mx, sum);
     }
     if (j + 1 < SETS) __syncthreads();
   }
-  __syncthreads();
-  if (left_out) add_left_out<BF16, PAGE>(a, p, u.kvh, rows, u.piece, max(from, least - least % BN), end);
+  if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
+  }
 }
 
 // The pieces of a row's context joined: W wavefronts a row, each takes its share of the pieces, a piece's maximum and sum
@@ -988,28 +974,50 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
-// How a call is cut up.  At most 64 rows a sequence and KV head go the thin way, 32 of them or two sets of 32 in a wavefront;
-// so do pages of less than 16 positions, 32 rows at a time, whatever the number of rows.  The context is cut into pieces
-// until there are `want` workgroups.
+constexpr int kThinGrid = 512;  // workgroups of a thin launch, at most
+
+// How a call is cut up.  At most 64 rows a sequence and KV head (32 in fp32) go the thin way, in one or two sets of 32; so do
+// pages of less than 16 positions, 32 rows at a time, whatever the number of rows.  The context is cut into pieces until
+// there are `want` workgroups: as many as the chip holds, and more where a batch's sequences may differ in length, which
+// is not known here.  Measured in us with as many / twice / eight times as many: one token of 16 sequences of 8K to 128K,
+// 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136; 5 tokens of 8 sequences of 4K to 64K in two sets
+// 186 / 101 / 95, 12 tokens of 2 sequences of 32K 62 / 75 / 97.
 struct Cut {
   int sets;  // thin: 1 or 2; 0: tiles of 128 rows
-  int tiles, pieces, piece;
+  int units, pieces, piece;
 };
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
   const int64_t most = (int64_t)s.n_max * G;
   Cut c;
-  c.sets = most <= 32 || s.page < 16 ? 1 : most <= 64 ? 2 : 0;
+  c.sets = most <= 32 || s.page < 16 ? 1 : most <= 64 && s.kv_dtype == LRQK_KV_BF16 ? 2 : 0;
   const int M = c.sets > 0 ? 32 * c.sets : 128;
   const int tiles = (int)(((int64_t)s.T * G + M - 1) / M);
-  c.tiles = tiles + s.B;  // no fewer than sum_b ceil(n_b G / M)
   const int64_t units = (int64_t)std::max(s.B, tiles) * s.Hkv;
-  const bool few = most <= 128;
-  const int64_t want = few ? 4096 : 512;
-  const int64_t pieces = (want + units - 1) / units;
-  const int64_t piece = std::max<int64_t>((s.l_max + pieces - 1) / pieces, few ? 256 : 1024);
+  // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
+  const int held = c.sets == 2 || (c.sets == 1 && s.kv_dtype == LRQK_KV_F32) ? 256 : 512;
+  int64_t pieces;
+  if (most <= 128) {
+    const int64_t want = (int64_t)held * (s.B == 1 ? 1 : c.sets == 1 ? 8 : 2);
+    pieces = (want + units - 1) / units;
+  } else {
+    // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths
+    pieces = 1;
+    double best = 0.0;
+    for (int n = 1; n <= 16; ++n) {
+      const double cost = (double)((units * n + held - 1) / held) / n * (1.0 + 0.04 * (n - 1));
+      if (n == 1 || cost < best) {
+        pieces = n;
+        best = cost;
+      }
+    }
+    // in a batch there may be sequences of few new tokens and a long context among the others
+    if (s.B > 1) pieces = std::max<int64_t>(pieces, (s.l_max + 32767) / 32768);
+  }
+  const int64_t piece = std::max<int64_t>((s.l_max + pieces - 1) / pieces, most <= 128 ? 256 : 512);
   c.piece = (int)((piece + 127) / 128 * 128);
   c.pieces = (s.l_max + c.piece - 1) / c.piece;
+  c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / M) times its pieces
   return c;
 }
 size_t partial_bytes(const lrqk_pages_shape& s) {
@@ -1030,12 +1038,14 @@ hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
 
 template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)c.tiles * s.Hkv * c.pieces));
+  const int most = std::max(1, kThinGrid / s.Hkv);
+  const dim3 grid((unsigned)(s.Hkv * (c.sets == 0 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
   if (s.page < 16) e = launch_thin<BF16, PAGE, 1, true>(grid, a, st);
   else if (c.sets == 1) e = launch_thin<BF16, PAGE, 1, false>(grid, a, st);
-  else if (c.sets == 2) e = launch_thin<BF16, PAGE, 2, false>(grid, a, st);
-  else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
+  else if (c.sets == 2) {
+    if constexpr (BF16) e = launch_thin<BF16, PAGE, 2, false>(grid, a, st);
+  } else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
   if (e != hipSuccess) return e;
   if (a.partials) {
     const int64_t rows = (int64_t)s.T * s.Hq;
@@ -1070,7 +1080,7 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   if (ws_bytes < lrqk_pages_workspace_bytes(shape)) return LRQK_ENOMEM;
   const Cut c = cut(s);
   const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
-               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.tiles, c.pieces, c.piece,
+               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.units, c.pieces, c.piece,
                (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(kD * page_elem_bytes(s.page_dtype) / 16), s.scale};
   hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {
