@@ -136,17 +136,30 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], uint32_t byte) {
   return make_uint2(w[0], w[1]);
 }
 
-// Sequence that packed row t belongs to, or -1; the whole wavefront asks, each lane for its own t: the
-// starts are read once, 64 at a time, without a chain of dependent loads.
-__device__ __forceinline__ int sequence_of(const Map& m, int t) {
+// Sequence that each packed row t belongs to, or -1; the whole wavefront asks, each lane for its own rows: the starts are
+// read once, 64 at a time, without a chain of dependent loads.
+template <int N>
+__device__ __forceinline__ void sequences_of(const Map& m, const int (&t)[N], int (&b)[N]) {
   const int lane = threadIdx.x & 63;
-  int b = 0;
+  const int first = m.start[0];
+#pragma unroll
+  for (int j = 0; j < N; ++j) b[j] = 0;
   for (int i0 = 0; i0 < m.B; i0 += 64) {
-    const int e = i0 + lane < m.B ? m.start[i0 + lane + 1] : INT32_MAX;
     const int todo = min(64, m.B - i0);
-    for (int j = 0; j < todo; ++j) b += __builtin_amdgcn_readlane(e, j) <= t ? 1 : 0;
+    const int e = m.start[i0 + min(lane, todo - 1) + 1];
+    for (int i = 0; i < todo; ++i) {
+      const int end = __builtin_amdgcn_readlane(e, i);
+#pragma unroll
+      for (int j = 0; j < N; ++j) b[j] += end <= t[j] ? 1 : 0;
+    }
   }
-  return b < m.B && t >= m.start[0] && t < m.T ? b : -1;
+#pragma unroll
+  for (int j = 0; j < N; ++j) b[j] = b[j] < m.B && t[j] >= first && t[j] < m.T ? b[j] : -1;
+}
+__device__ __forceinline__ int sequence_of(const Map& m, int t) {
+  int b[1];
+  sequences_of(m, {t}, b);
+  return b[0];
 }
 
 // f(bf16 dense rows, page type) for the five combinations that check_pages lets through

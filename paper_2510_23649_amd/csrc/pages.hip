@@ -1,10 +1,7 @@
 // g1, g2 -- the paged K/V cache is written and read back (include/lrqk.h).
 //
-// Both move rows of 128 elements and are bound by memory.  16 lanes share a row, 8 elements each: 16-byte
-// loads and stores of bf16 rows, full rows of 256 bytes per 16 lanes.  An 8-bit row has its four
-// blocks of 32 elements in four lanes each: the block's largest magnitude takes two DPP steps, its
-// scale is a power of two read off the bits (see pages.h), so that nothing but the rounding to the
-// code is rounded.
+// Both move rows of 128 elements and are bound by memory: by its latency where a lane has one row in flight, by its
+// bandwidth with several.
 #include "pages.h"
 
 #include <cmath>
@@ -45,114 +42,145 @@ namespace {
 using namespace pages;
 
 constexpr int kMoveThreads = 256;
-constexpr int kRowsPerBlock = kMoveThreads / 16;
 
-// Eight elements of a row, chunk c of 16.
+// ---- g1 ----------------------------------------------------------------------------------------------------
+constexpr int kAppendEach = 4;                                   // rows of K and of V a 16-lane group has in flight
+constexpr int kAppendRows = kMoveThreads / 16 * kAppendEach;     // rows of K (and of V) a workgroup
+
+// Eight elements of a row, chunk c of 16, as they are, and as fp32.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t row, int c, float (&x)[8]) {
-  if constexpr (BF16) {
-    const uint4 u = static_cast<const uint4*>(base)[row * 16 + c];
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void load8(const void* base, int64_t row, int c, uint4& a, uint4& b) {
+  const uint4* p = static_cast<const uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
+  a = p[0];
+  if (!BF16) b = p[1];
+}
+template <bool BF16>
+__device__ __forceinline__ void store8(void* base, int64_t row, int c, uint4 a, uint4 b) {
+  uint4* p = static_cast<uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
+  p[0] = a;
+  if (!BF16) p[1] = b;
+}
+template <bool BF16>
+__device__ __forceinline__ void get8(uint4 a, uint4 b, float (&x)[8]) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-    const float4 a = static_cast<const float4*>(base)[(row * 16 + c) * 2];
-    const float4 b = static_cast<const float4*>(base)[(row * 16 + c) * 2 + 1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-}
-template <bool BF16>
-__device__ __forceinline__ void store8(void* base, int64_t row, int c, const float (&x)[8]) {
-  if constexpr (BF16) {
-    static_cast<uint4*>(base)[row * 16 + c] =
-        make_uint4(dev::pack_bf16(x[0], x[1]), dev::pack_bf16(x[2], x[3]), dev::pack_bf16(x[4], x[5]),
-                   dev::pack_bf16(x[6], x[7]));
-  } else {
-    static_cast<float4*>(base)[(row * 16 + c) * 2] = make_float4(x[0], x[1], x[2], x[3]);
-    static_cast<float4*>(base)[(row * 16 + c) * 2 + 1] = make_float4(x[4], x[5], x[6], x[7]);
-  }
+  for (int i = 0; i < 8; ++i)
+    x[i] = __uint_as_float(!BF16 ? w[i] : i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xffff0000u);
 }
 
-// One 16-lane group per row of k_new (blockIdx.y == 0) or v_new (1).
+// A 16-lane group takes rows of k_new and v_new, 8 elements a lane; the rows are on their way while their places are found.
+// An 8-bit row has its four blocks of 32 elements in four lanes each: a block's largest magnitude takes two DPP steps.
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kMoveThreads) void pages_append_kernel(const Map m, const void* k_new,
                                                                     const void* v_new, void* K, void* V,
                                                                     uint8_t* K_scale, uint8_t* V_scale) {
   const int grp = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const void* src = blockIdx.y ? v_new : k_new;
-  void* dst = blockIdx.y ? V : K;
-  uint8_t* sc = blockIdx.y ? V_scale : K_scale;
   const int64_t rows = (int64_t)m.T * m.Hkv;
-  for (int64_t r0 = (int64_t)blockIdx.x * kRowsPerBlock; r0 < rows; r0 += (int64_t)gridDim.x * kRowsPerBlock) {
-    const int64_t r = r0 + grp;
-    const int t = (int)min(r / m.Hkv, (int64_t)m.T), kvh = (int)(r % m.Hkv);
-    const int b = sequence_of(m, t);  // the whole wavefront takes part
-    if (b < 0) continue;
-    const Seq q = sequence(m, b);
-    if (t < q.first || t >= q.first + q.n) continue;
-    const int p = q.len - q.n + (t - q.first);
-    if (p < 0 || p >= m.l_max) continue;
-    const int64_t row = row_of(m, b, kvh, p);
-    if (row < 0) continue;
-    if constexpr (!is8(PAGE)) {
-      constexpr int kChunks = BF16 ? 1 : 2;
+  for (int64_t r0 = (int64_t)blockIdx.x * kAppendRows; r0 < rows; r0 += (int64_t)gridDim.x * kAppendRows) {
+    uint4 k[kAppendEach], v[kAppendEach], k2[kAppendEach], v2[kAppendEach];  // (2: fp32 rows only)
+    int t[kAppendEach], b[kAppendEach];
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i)
-        static_cast<uint4*>(dst)[(row * 16 + c) * kChunks + i] =
-            static_cast<const uint4*>(src)[(r * 16 + c) * kChunks + i];
-    } else {
-      float x[8];
-      load8<BF16>(src, r, c, x);
-      uint32_t top = 0;
+    for (int j = 0; j < kAppendEach; ++j) {
+      const int64_t r = min(r0 + j * (kMoveThreads / 16) + grp, rows - 1);
+      k2[j] = v2[j] = make_uint4(0, 0, 0, 0);
+      load8<BF16>(k_new, r, c, k[j], k2[j]);
+      load8<BF16>(v_new, r, c, v[j], v2[j]);
+      t[j] = (int)((uint32_t)r / (uint32_t)m.Hkv);
+    }
+    sequences_of(m, t, b);  // the whole wavefront takes part
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-      top = max(top, dev::dpp_u32<0xB1>(top));  // over the four lanes of a block
-      top = max(top, dev::dpp_u32<0x4E>(top));
-      const uint32_t byte = scale_byte<PAGE>(top);
-      static_cast<uint2*>(dst)[row * 16 + c] = encode8<PAGE>(x, byte);
-      if ((c & 3) == 0) sc[row * kScales + (c >> 2)] = (uint8_t)byte;
+    for (int j = 0; j < kAppendEach; ++j) {
+      const int64_t r = r0 + j * (kMoveThreads / 16) + grp;
+      if (r >= rows || b[j] < 0) continue;
+      const Seq q = sequence(m, b[j]);
+      const int p = q.len - q.n + (t[j] - q.first);
+      if (t[j] < q.first || t[j] >= q.first + q.n || p < 0 || p >= m.l_max) continue;
+      const int64_t row = row_of(m, b[j], (int)((uint32_t)r % (uint32_t)m.Hkv), p);
+      if (row < 0) continue;
+      if constexpr (!is8(PAGE)) {
+        store8<BF16>(K, row, c, k[j], k2[j]);
+        store8<BF16>(V, row, c, v[j], v2[j]);
+      } else {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          float x[8];
+          get8<BF16>(which ? v[j] : k[j], which ? v2[j] : k2[j], x);
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+          top = max(top, dev::dpp_u32<0xB1>(top));  // over the four lanes of a block
+          top = max(top, dev::dpp_u32<0x4E>(top));
+          const uint32_t byte = scale_byte<PAGE>(top);
+          static_cast<uint2*>(which ? V : K)[row * 16 + c] = encode8<PAGE>(x, byte);
+          if ((c & 3) == 0) (which ? V_scale : K_scale)[row * kScales + (c >> 2)] = (uint8_t)byte;
+        }
+      }
     }
   }
 }
 
-// One 16-lane group per position; K and V of it.  Workgroups: (sequence, stretch of positions, KV head).
+// ---- g2 ----------------------------------------------------------------------------------------------------
+constexpr int kReadSpan = 32;  // positions of a workgroup
+
+// Workgroups: (KV head, stretch of positions, sequence).  All rows of K and V of a workgroup are on their way before the first
+// is stored.  A lane makes 16 bytes of a dense row, so that the wavefront's stores are whole, and they are streamed past
+// the caches.  A prompt of 32K, e4m3 to bf16 (204 MB): 31 us, 6.6 TB/s; with ordinary stores 43, with lanes that make
+// 32 bytes in two stores 50 (66 streamed: halves of lines).
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kMoveThreads) void pages_read_kernel(const Map m, const void* K, const void* V,
                                                                   const uint8_t* K_scale,
                                                                   const uint8_t* V_scale, int first,
                                                                   int stretches, int64_t units, int lrows,
                                                                   void* K_out, void* V_out) {
-  const int grp = threadIdx.x >> 4, c = threadIdx.x & 15;
+  constexpr int kLanes = kD * (BF16 ? 2 : 4) / 16, kPass = kMoveThreads / kLanes, kN = kReadSpan / kPass;
+  using Raw = std::conditional_t<!is8(PAGE), uint4, std::conditional_t<BF16, uint2, uint32_t>>;
+  const int grp = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int kvh = (int)(u % m.Hkv);
     const int64_t v = u / m.Hkv;
-    const int b = (int)(v / stretches), st = (int)(v % stretches);
-    const int p = first + st * kRowsPerBlock + grp;
+    const int b = (int)(v / stretches), p0 = first + (int)(v % stretches) * kReadSpan;
     const int len = min(m.kv_len[b], m.l_max);
-    if (p >= len) continue;
-    const int64_t row = row_of(m, b, kvh, p);
-    if (row < 0) continue;
-    const int64_t to = ((int64_t)b * m.Hkv + kvh) * lrows + p;
+    if (p0 >= len) continue;
+    int64_t row[kN];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int p = p0 + i * kPass + grp;
+      row[i] = row_of(m, b, kvh, min(p, len - 1));
+      if (p >= len) row[i] = -1;
+    }
+    Raw x[2][kN];
+    uint32_t sc[2][kN];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      const void* src = which ? V : K;
-      void* dst = which ? V_out : K_out;
-      if (!dst) continue;
-      if constexpr (!is8(PAGE)) {
-        constexpr int kChunks = BF16 ? 1 : 2;
+      if (!(which ? V_out : K_out)) continue;
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i)
-          static_cast<uint4*>(dst)[(to * 16 + c) * kChunks + i] =
-              static_cast<const uint4*>(src)[(row * 16 + c) * kChunks + i];
-      } else {
-        const uint8_t* sc = which ? V_scale : K_scale;
-        float x[8];
-        decode8<PAGE>(static_cast<const uint2*>(src)[row * 16 + c], scale_of(sc[row * kScales + (c >> 2)]), x);
-        store8<BF16>(dst, to, c, x);
+      for (int i = 0; i < kN; ++i) {
+        if (row[i] < 0) continue;
+        x[which][i] = static_cast<const Raw*>(which ? V : K)[row[i] * kLanes + c];
+        if constexpr (is8(PAGE)) sc[which][i] = (which ? V_scale : K_scale)[row[i] * kScales + c / (kLanes / kScales)];
+      }
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      void* const out = which ? V_out : K_out;
+      if (!out) continue;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        if (row[i] < 0) continue;
+        uint4 y;
+        if constexpr (!is8(PAGE)) {
+          y = x[which][i];
+        } else if constexpr (BF16) {
+          y = decode8_bf16<PAGE>(x[which][i], scale_of(sc[which][i]));
+        } else {
+          float f[8];
+          decode8<PAGE>(make_uint2(x[which][i], 0u), scale_of(sc[which][i]), f);
+          y = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        }
+        const dev::u32x4 z = {y.x, y.y, y.z, y.w};
+        __builtin_nontemporal_store(
+            z, reinterpret_cast<dev::u32x4*>(out) +
+                   (((int64_t)b * m.Hkv + kvh) * lrows + p0 + i * kPass + grp) * kLanes + c);
       }
     }
   }
@@ -175,8 +203,8 @@ LRQK_API int lrqk_pages_append(const lrqk_pages_shape* shape, const lrqk_pages* 
   const lrqk_pages_shape& s = *shape;
   if (!pages_given(s, pg) || !k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return LRQK_EINVAL;
   const Map m = make_map(s, *pg);
-  const int64_t blocks = ((int64_t)s.T * s.Hkv + kRowsPerBlock - 1) / kRowsPerBlock;
-  const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), 2);
+  const int64_t blocks = ((int64_t)s.T * s.Hkv + kAppendRows - 1) / kAppendRows;
+  const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
   by_type(s, [&](auto bf16, auto page) {
     hipLaunchKernelGGL((pages_append_kernel<bf16.value, page.value>), grid, dim3(kMoveThreads), 0,
                        static_cast<hipStream_t>(stream), m, k_new, v_new, pg->K, pg->V, pg->K_scale,
@@ -196,7 +224,7 @@ LRQK_API int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pg
   if ((K_out && !aligned16(K_out)) || (V_out && !aligned16(V_out))) return LRQK_EINVAL;
   if (first >= s.l_max) return LRQK_OK;  // no such position
   const Map m = make_map(s, *pg);
-  const int stretches = ceil_div(s.l_max - first, kRowsPerBlock);
+  const int stretches = ceil_div(s.l_max - first, kReadSpan);
   const int64_t units = (int64_t)s.B * s.Hkv * stretches;
   const dim3 grid((unsigned)(units < kMostBlocks ? units : kMostBlocks));
   by_type(s, [&](auto bf16, auto page) {
