@@ -218,21 +218,24 @@ struct Block {
   static __device__ __forceinline__ void load(const Args& a, int b, int kvh, int end, const void* base,
                                               const uint8_t* scale, const Found& f, int lane, Held& r) {
     const int c = lane % kLanes;
-    uint32_t at[kN];
     if constexpr (SMALL) {
+      uint32_t at[kN];
       find_rows(a, b, kvh, f.p0, end, lane, at);
-    } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        const int g = i * kPass / kGroup;
-        at[i] = f.place[g] + (uint32_t)(row_in_wave(i, lane) - g * kGroup) * kRow16;
+        r.x[i] = static_cast<const uint4*>(base)[(size_t)(at[i] + c)];
+        if constexpr (is8(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) >> 1)];
       }
-    }
+    } else {
+      // first what all lanes share, then what a lane adds in every block, then a number that the instruction holds
+      const uint32_t mine = (uint32_t)(lane / kLanes * kRow16 + c);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      r.x[i] = static_cast<const uint4*>(base)[(size_t)(at[i] + c)];
-      // 16 codes are half a scale block; a row has 8 chunks and 4 scales
-      if constexpr (is8(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) >> 1)];
+      for (int i = 0; i < kN; ++i) {
+        const int g = i * kPass / kGroup, rows = i * kPass - g * kGroup;
+        r.x[i] = (static_cast<const uint4*>(base) + (size_t)f.place[g])[mine + rows * kRow16];
+        // 16 codes are half a scale block; a row has 8 chunks and 4 scales
+        if constexpr (is8(PAGE)) r.scale[i] = (scale + ((size_t)f.place[g] >> 1))[(mine >> 1) + rows * kScales];
+      }
     }
   }
 
@@ -701,18 +704,20 @@ struct TileLoop {
   }
 };
 
-// The rounds of a tile in fp32: blocks of 32 positions, the next one on its way.
-template <int PAGE>
-struct TileLoopF32 {
-  static constexpr int BN = 32;
-  using B = Block<false, PAGE, BN, kWaves>;
+// Rounds without a pipeline of steps, the next block on its way: tiles in fp32, which take blocks of 32 positions, and pairs,
+// where a wavefront attends to one half of a block of 64.
+template <bool BF16, int PAGE, int BLOCK>
+struct PlainLoop {
+  static constexpr int BN = BLOCK;
+  using B = Block<BF16, PAGE, BN, kWaves>;
   const Args& a;
   const Problem& p;
   int kvh, w, lane, from, end, least, my_least;
   bool busy, cleared;
   float c;
-  Rows<false>& r;
+  Rows<BF16>& r;
   uint16_t (*there)[4];
+  int half;  // of the block that the wavefront attends to
   B blk;
   typename B::Found f;
   typename B::Held hk, hv;
@@ -746,7 +751,10 @@ struct TileLoopF32 {
     }
     __syncthreads();
     if (p0 + BN < end) fetch(p0 + BN, kt_to, vt_to, bits_to);
-    if (busy) r.attend(kt, vt, p0, (uint32_t)gather_there<8>(bits), p0 + BN <= my_least, c, lane);
+    const int off = 32 * half;
+    if (busy)
+      r.attend(kt + off * kRowB<BF16>, vt + off * kRowB<BF16>, p0 + off, (uint32_t)(gather_there<BN / kWaves>(bits) >> off),
+               p0 + off + 32 <= my_least, c, lane);
   }
   __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
     blk.look_up(a.m, p.b, from + w * B::kMine, end);
@@ -760,7 +768,7 @@ struct TileLoopF32 {
 
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
-  using Loop = std::conditional_t<BF16, TileLoop<PAGE>, TileLoopF32<PAGE>>;
+  using Loop = std::conditional_t<BF16, TileLoop<PAGE>, PlainLoop<false, PAGE, 32>>;
   constexpr int M = 128, BN = Loop::BN, kTile = BN * kRowB<BF16>;
   __shared__ __align__(16) char kt0[kTile], vt0[kTile], kt1[kTile], vt1[kTile];
   __shared__ __align__(8) uint16_t there[4][4];
@@ -797,100 +805,136 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
 }
 
-template <bool BF16, int PAGE, int SETS, bool SMALL>
-__global__ __launch_bounds__(kThreads, BF16 && SETS == 1 ? 2 : 1) void attend_thin_kernel(const Args a) {
-  constexpr int M = 32 * SETS, BN = 32;
+// The states of several wavefronts at the same rows joined and put: `n` of them, that of state v and row i at
+// acc[(v * rows_held + i) * 128], its 16-byte chunks turned by i % 32, its maximum and sum at mx[v * rows_held + i] and sum[..].
+template <bool BF16>
+__device__ __forceinline__ void join_states(const Args& a, const Problem& p, int kvh, int rows, int n, int rows_held,
+                                            const float* acc, const float* wm, const float* ws) {
+  for (int k = threadIdx.x; k < rows * (kD / 4); k += kThreads) {
+    const int row = k / (kD / 4), chunk = k % (kD / 4);
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    float mx = -INFINITY, sum = 0.0f;
+    for (int v = 0; v < n; ++v) mx = fmaxf(mx, wm[v * rows_held + row]);
+    for (int v = 0; v < n; ++v) {
+      const int i = v * rows_held + row;
+      const float f = weight_of(wm[i], ws[i], mx);
+      sum += ws[i] * f;
+      const f32x4 y = *reinterpret_cast<const f32x4*>(acc + (size_t)i * kD + 4 * (chunk ^ (row & 31)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, y[e], x[e]);
+    }
+    put<BF16>(a, p, kvh, p.r0 + row, p.piece, 4 * chunk, x, mx, sum);
+  }
+}
+// A wavefront's state as state v, rows i0 .. i0 + 31, of those.
+template <bool BF16>
+__device__ __forceinline__ void leave_state(const Rows<BF16>& r, int at, int lane, float* acc, float* wm, float* ws) {
+  const int i = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4*>(acc + (size_t)(at + i) * kD + 4 * ((8 * t + 2 * e + h) ^ i)) =
+          f32x4{r.o[t][4 * e], r.o[t][4 * e + 1], r.o[t][4 * e + 2], r.o[t][4 * e + 3]};
+  const float sum = sum_halves(r.sum);
+  if (h == 0) {
+    wm[at + i] = r.mx;
+    ws[at + i] = sum;
+  }
+}
+
+template <bool BF16, int PAGE, bool SMALL>
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(const Args a) {
+  constexpr int M = 32, BN = 32;
   constexpr int kTile = BN * kRowB<BF16>;
   extern __shared__ __align__(16) char lds[];  // per wavefront: K, V
-  __shared__ float wm[kWaves][M], ws[kWaves][M];
+  __shared__ float wm[kWaves * M], ws[kWaves * M];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % a.m.Hkv;
   // the grid is as large as the chip: how many units there are is known here alone
   for (int unit = blockIdx.x / a.m.Hkv;; unit += gridDim.x / a.m.Hkv) {
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
-  Problem p;
-  if (!find_unit<M>(a, unit, p)) return;
-  const int rows = min(M, p.rows - p.r0);
-  const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-  const int from = p.piece * a.piece, end = min(most, from + a.piece);
-  if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
-  Rows<BF16> r[SETS];
-#pragma unroll
-  for (int j = 0; j < SETS; ++j) {
-    const int real = min(p.r0 + 32 * j + (lane & 31), p.rows - 1);
-    r[j].see = sees(a, p, real);
-    r[j].start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
-  }
-  const float c = log2_scale(a);
-  char* const kt = lds + w * 2 * kTile;
-  char* const vt = kt + kTile;
-  bool cleared = false;
-  const int mine = from + w * BN;
-  if (mine < end) {
-    using B = Block<BF16, PAGE, BN, 1, SMALL>;
-    B blk;
-    typename B::Found f;
-    typename B::Held hk, hv;
-    auto fetch = [&](int p0) __attribute__((always_inline)) {
-      blk.find(a, p.b, kvh, p0, end, lane, f);
-      B::load(a, p.b, kvh, end, a.K, a.K_scale, f, lane, hk);
-      B::load(a, p.b, kvh, end, a.V, a.V_scale, f, lane, hv);
-      blk.look_up(a.m, p.b, p0 + kWaves * BN, end);
-    };
-    blk.look_up(a.m, p.b, mine, end);
-    fetch(mine);
-    for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
-      __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
-      B::store_k(hk, 0, lane, kt);
-      cleared |= B::store_v(hv, f.there, p0 + BN > least, 0, lane, vt);
-      __builtin_amdgcn_wave_barrier();
-      const uint32_t there = f.there;
-      if (p0 + kWaves * BN < end) fetch(p0 + kWaves * BN);
-#pragma unroll
-      for (int j = 0; j < SETS; ++j) r[j].attend(kt, vt, p0, there, p0 + BN <= least, c, lane);
-    }
-  }
-  // merge the four states: the accumulators, at a common maximum, meet in LDS, 32 rows at a time
-#pragma unroll
-  for (int j = 0; j < SETS; ++j) {
-    r[j].sum = sum_halves(r[j].sum);
-    if (lane < 32) {
-      wm[w][32 * j + lane] = r[j].mx;
-      ws[w][32 * j + lane] = r[j].sum;
-    }
-  }
-  __syncthreads();
-  const int i = lane & 31, h = lane >> 5;
-  float* const acc = reinterpret_cast<float*>(lds);  // [wave][row][128], 16-byte chunks turned by the row
-#pragma unroll
-  for (int j = 0; j < SETS; ++j) {
-    const int r0 = 32 * j;
-    const float top = fmaxf(fmaxf(wm[0][r0 + i], wm[1][r0 + i]), fmaxf(wm[2][r0 + i], wm[3][r0 + i]));
-    const float f = weight_of(r[j].mx, r[j].sum, top);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4*>(acc + (w * 32 + i) * kD + 4 * ((8 * t + 2 * e + h) ^ i)) =
-            f32x4{r[j].o[t][4 * e] * f, r[j].o[t][4 * e + 1] * f, r[j].o[t][4 * e + 2] * f, r[j].o[t][4 * e + 3] * f};
-    __syncthreads();
-    for (int k = threadIdx.x; k < min(32, rows - r0) * (kD / 4); k += kThreads) {
-      const int row = k / (kD / 4), chunk = k % (kD / 4);
-      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-      float mx = -INFINITY, sum = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, wm[v][r0 + row]);
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        sum += ws[v][r0 + row] * weight_of(wm[v][r0 + row], ws[v][r0 + row], mx);
-        x += *reinterpret_cast<const f32x4*>(acc + (v * 32 + row) * kD + 4 * (chunk ^ row));
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
+    Problem p;
+    if (!find_unit<M>(a, unit, p)) return;
+    const int rows = min(M, p.rows - p.r0);
+    const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
+    const int from = p.piece * a.piece, end = min(most, from + a.piece);
+    if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
+    Rows<BF16> r;
+    const int real = min(p.r0 + (lane & 31), p.rows - 1);
+    r.see = sees(a, p, real);
+    r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    const float c = log2_scale(a);
+    char* const kt = lds + w * 2 * kTile;
+    char* const vt = kt + kTile;
+    bool cleared = false;
+    const int mine = from + w * BN;
+    if (mine < end) {
+      using B = Block<BF16, PAGE, BN, 1, SMALL>;
+      B blk;
+      typename B::Found f;
+      typename B::Held hk, hv;
+      auto fetch = [&](int p0) __attribute__((always_inline)) {
+        blk.find(a, p.b, kvh, p0, end, lane, f);
+        B::load(a, p.b, kvh, end, a.K, a.K_scale, f, lane, hk);
+        B::load(a, p.b, kvh, end, a.V, a.V_scale, f, lane, hv);
+        blk.look_up(a.m, p.b, p0 + kWaves * BN, end);
+      };
+      blk.look_up(a.m, p.b, mine, end);
+      fetch(mine);
+      for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
+        __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
+        B::store_k(hk, 0, lane, kt);
+        cleared |= B::store_v(hv, f.there, p0 + BN > least, 0, lane, vt);
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t there = f.there;
+        if (p0 + kWaves * BN < end) fetch(p0 + kWaves * BN);
+        r.attend(kt, vt, p0, there, p0 + BN <= least, c, lane);
       }
-      put<BF16>(a, p, kvh, p.r0 + r0 + row, p.piece, 4 * chunk, x, mx, sum);
     }
-    if (j + 1 < SETS) __syncthreads();
+    __syncthreads();  // (in fp32 a state lies where another wavefront's rows were)
+    leave_state(r, w * M, lane, reinterpret_cast<float*>(lds), wm, ws);
+    __syncthreads();
+    join_states<BF16>(a, p, kvh, rows, kWaves, M, reinterpret_cast<const float*>(lds), wm, ws);
+    if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
   }
-  if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
+}
+
+template <int PAGE>
+__global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) {
+  using Loop = PlainLoop<true, PAGE, 64>;
+  constexpr int M = 64, BN = Loop::BN, kTile = BN * kRowB<true>;
+  __shared__ __align__(16) char lds[4 * kTile];  // two buffers of K and V; then the states
+  __shared__ __align__(8) uint16_t there[4][4];
+  __shared__ float wm[2 * M], ws[2 * M];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), set = w & 1, half = w >> 1;
+  const int kvh = blockIdx.x % a.m.Hkv;
+  for (int unit = blockIdx.x / a.m.Hkv;; unit += gridDim.x / a.m.Hkv) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // (as above)
+    Problem p;
+    if (!find_unit<M>(a, unit, p)) return;
+    const int rows = min(M, p.rows - p.r0);
+    const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
+    const int from = p.piece * a.piece, end = min(most, from + a.piece);
+    if (from >= end && p.piece > 0) continue;
+    Rows<true> r;
+    const int real = min(p.r0 + 32 * set + (lane & 31), p.rows - 1);
+    r.see = sees(a, p, real);
+    r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    bool cleared = false;
+    if (from < end) {
+      Loop loop{a,     p,    kvh, w, lane, from, end, least, sees(a, p, min(p.r0 + 32 * set, p.rows - 1)), 32 * set < rows,
+                false, log2_scale(a), r, there, half};
+      loop.run(lds, lds + kTile, lds + 2 * kTile, lds + 3 * kTile);
+      cleared = loop.cleared;
+    }
+    __syncthreads();
+    leave_state(r, half * M + 32 * set, lane, reinterpret_cast<float*>(lds), wm, ws);
+    __syncthreads();
+    join_states<true>(a, p, kvh, rows, 2, M, reinterpret_cast<const float*>(lds), wm, ws);
+    if (__syncthreads_or(cleared)) add_left_out<true, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
   }
 }
 
@@ -974,7 +1018,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
-constexpr int kThinGrid = 512;  // workgroups of a thin launch, at most
+constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
 // How a call is cut up.  At most 64 rows a sequence and KV head (32 in fp32) go the thin way, in one or two sets of 32; so do
 // pages of less than 16 positions, 32 rows at a time, whatever the number of rows.  The context is cut into pieces until
@@ -983,22 +1027,21 @@ constexpr int kThinGrid = 512;  // workgroups of a thin launch, at most
 // 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136; 5 tokens of 8 sequences of 4K to 64K in two sets
 // 186 / 101 / 95, 12 tokens of 2 sequences of 32K 62 / 75 / 97.
 struct Cut {
-  int sets;  // thin: 1 or 2; 0: tiles of 128 rows
+  int rows;  // 32: thin, 64: pair, 128: tile
   int units, pieces, piece;
 };
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
   const int64_t most = (int64_t)s.n_max * G;
   Cut c;
-  c.sets = most <= 32 || s.page < 16 ? 1 : most <= 64 && s.kv_dtype == LRQK_KV_BF16 ? 2 : 0;
-  const int M = c.sets > 0 ? 32 * c.sets : 128;
-  const int tiles = (int)(((int64_t)s.T * G + M - 1) / M);
+  c.rows = most <= 32 || s.page < 16 ? 32 : most <= 64 && s.kv_dtype == LRQK_KV_BF16 ? 64 : 128;
+  const int tiles = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows);
   const int64_t units = (int64_t)std::max(s.B, tiles) * s.Hkv;
   // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
-  const int held = c.sets == 2 || (c.sets == 1 && s.kv_dtype == LRQK_KV_F32) ? 256 : 512;
+  const int held = c.rows == 32 && s.kv_dtype == LRQK_KV_F32 ? 256 : 512;
   int64_t pieces;
   if (most <= 128) {
-    const int64_t want = (int64_t)held * (s.B == 1 ? 1 : c.sets == 1 ? 8 : 2);
+    const int64_t want = (int64_t)held * (s.B == 1 ? 1 : c.rows == 32 ? 8 : 2);
     pieces = (want + units - 1) / units;
   } else {
     // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths
@@ -1017,7 +1060,7 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t piece = std::max<int64_t>((s.l_max + pieces - 1) / pieces, most <= 128 ? 256 : 512);
   c.piece = (int)((piece + 127) / 128 * 128);
   c.pieces = (s.l_max + c.piece - 1) / c.piece;
-  c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / M) times its pieces
+  c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / rows) times its pieces
   return c;
 }
 size_t partial_bytes(const lrqk_pages_shape& s) {
@@ -1025,11 +1068,11 @@ size_t partial_bytes(const lrqk_pages_shape& s) {
   return c.pieces > 1 ? (size_t)s.T * s.Hq * c.pieces * kPartial * sizeof(float) : 0;
 }
 
-template <bool BF16, int PAGE, int SETS, bool SMALL>
+template <bool BF16, int PAGE, bool SMALL>
 hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
   constexpr size_t kLds = (size_t)kWaves * 2 * 32 * kRowB<BF16>;
   static std::atomic<uint64_t> done{0};
-  const auto kernel = attend_thin_kernel<BF16, PAGE, SETS, SMALL>;
+  const auto kernel = attend_thin_kernel<BF16, PAGE, SMALL>;
   const hipError_t e = raise_dynamic_lds_once(kernel, kLds, done);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLds, st, a);
@@ -1038,13 +1081,13 @@ hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
 
 template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
-  const int most = std::max(1, kThinGrid / s.Hkv);
-  const dim3 grid((unsigned)(s.Hkv * (c.sets == 0 ? c.units : std::min(c.units, most))));
+  const int most = std::max(1, kFewGrid / s.Hkv);
+  const dim3 grid((unsigned)(s.Hkv * (c.rows == 128 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
-  if (s.page < 16) e = launch_thin<BF16, PAGE, 1, true>(grid, a, st);
-  else if (c.sets == 1) e = launch_thin<BF16, PAGE, 1, false>(grid, a, st);
-  else if (c.sets == 2) {
-    if constexpr (BF16) e = launch_thin<BF16, PAGE, 2, false>(grid, a, st);
+  if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
+  else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
+  else if (c.rows == 64) {
+    if constexpr (BF16) hipLaunchKernelGGL((attend_pair_kernel<PAGE>), grid, dim3(kThreads), 0, st, a);
   } else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
   if (e != hipSuccess) return e;
   if (a.partials) {
