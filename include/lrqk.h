@@ -460,8 +460,8 @@ enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 =
 
 /*
  *   T          rows of the packed arrays (q, out, k_new, v_new), 1 <= T < 2^24
- *   n_max      new tokens of any one sequence, at most; chooses between kernels, results do not
- *              depend on it
+ *   n_max      new tokens of any one sequence, at most; chooses between kernels, whose results
+ *              differ by roundings
  *   l_max      positions of any one sequence, at most, 1 <= l_max < 2^24
  *   l_cap      rows allocated per head in the dense arrays of lrqk_pages_read; 0 means l_max
  *   page       positions per page: a power of two, 1 <= page <= 1024

@@ -380,6 +380,9 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
     p = Pages(_dev(K), _dev(V), _dev(K_scale, torch.uint8), _dev(V_scale, torch.uint8),
               _dev(table, torch.int32), _dev(start, torch.int32), _dev(kv_len, torch.int32))
     p.tensors = (K, V, K_scale, V_scale, table, start, kv_len)
+    p.device = K.device.index
+    if any(t is not None and t.device.index != p.device for t in p.tensors):
+        raise ValueError("pages on several devices")
     return p
 
 
@@ -401,8 +404,11 @@ def _fits(t: Optional[torch.Tensor], shape: PagesShape, rows: int, pinned=False)
     return ptr
 
 
-def _raw_stream(stream) -> Optional[int]:
-    """As _stream; the current one without the object around it (3 us of a call of 9)."""
+def _raw_stream(stream, pages: Pages) -> Optional[int]:
+    """As _stream, for a call on `pages`; the current one without the object around it (3 us of a call of 9)."""
+    device = getattr(pages, "device", None)
+    if device is not None and device != torch.cuda.current_device():
+        raise ValueError(f"pages on device {device}, current device is {torch.cuda.current_device()}")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return _stream(stream)
@@ -412,7 +418,7 @@ def lrqk_pages_append(shape, pages, k_new, v_new, stream=None):
     rows = shape.T * shape.Hkv
     _check(load_library().lrqk_pages_append(C.byref(shape), C.byref(pages),
                                             _fits(k_new, shape, rows), _fits(v_new, shape, rows),
-                                            _raw_stream(stream)), "lrqk_pages_append")
+                                            _raw_stream(stream, pages)), "lrqk_pages_append")
 
 
 def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
@@ -420,12 +426,14 @@ def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
     _check(load_library().lrqk_pages_read(C.byref(shape), C.byref(pages), int(first),
                                           _fits(K_out, shape, rows, pinned=True),
                                           _fits(V_out, shape, rows, pinned=True),
-                                          _raw_stream(stream)), "lrqk_pages_read")
+                                          _raw_stream(stream, pages)), "lrqk_pages_read")
 
 
 def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
     rows = shape.T * shape.Hq
+    if workspace.device != out.device:
+        raise ValueError(f"workspace on {workspace.device}, out on {out.device}")
     _check(load_library().lrqk_chunk_attend(
         C.byref(shape), C.byref(pages), _fits(q, shape, rows), _fits(out, shape, rows),
-        _dev(workspace), workspace.numel() * workspace.element_size(), _raw_stream(stream)),
+        _dev(workspace), workspace.numel() * workspace.element_size(), _raw_stream(stream, pages)),
         "lrqk_chunk_attend")

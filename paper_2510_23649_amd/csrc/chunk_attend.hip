@@ -87,6 +87,7 @@ __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
       p.s.n = __builtin_amdgcn_readlane(n, j);
       p.s.len = __builtin_amdgcn_readlane(len, j);
       p.rows = p.s.n * a.G;
+      if (mine < 0) return false;  // (no start may send a workgroup anywhere)
       // the last tiles of a sequence see most: they come first
       const int back = __builtin_amdgcn_readlane(units, j) - 1 - mine;
       p.piece = back / t;
@@ -562,7 +563,8 @@ __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows,
       if (at < 0) continue;
       float v;
       if constexpr (is8(PAGE)) {
-        v = a.V_scale[at * kScales + d / kScaleBlock] == 255 ? NAN : 0.0f;
+        const bool nan = PAGE == LRQK_PAGE_E4M3 && (static_cast<const uint8_t*>(a.V)[at * kD + d] & 0x7f) == 0x7f;
+        v = nan || a.V_scale[at * kScales + d / kScaleBlock] == 255 ? NAN : 0.0f;
       } else if constexpr (PAGE == LRQK_PAGE_BF16) {
         v = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.V)[at * kD + d] << 16);
       } else {
@@ -1020,12 +1022,13 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
-// How a call is cut up.  At most 64 rows a sequence and KV head (32 in fp32) go the thin way, in one or two sets of 32; so do
-// pages of less than 16 positions, 32 rows at a time, whatever the number of rows.  The context is cut into pieces until
-// there are `want` workgroups: as many as the chip holds, and more where a batch's sequences may differ in length, which
-// is not known here.  Measured in us with as many / twice / eight times as many: one token of 16 sequences of 8K to 128K,
-// 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136; 5 tokens of 8 sequences of 4K to 64K in two sets
-// 186 / 101 / 95, 12 tokens of 2 sequences of 32K 62 / 75 / 97.
+// How a call is cut up.  At most 32 rows a sequence and KV head go the thin way, and all calls with pages of less than 16
+// positions; up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit); more in tiles.  Where
+// there are few rows, the context is cut until there are `want` workgroups: as many as the chip holds, and more where a
+// batch's sequences may differ in length, which is not known here.  Measured in us with as many / twice / eight times as
+// many: one token of 16 sequences of 8K to 128K, 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136;
+// pairs, with as many / twice / four times: 5 tokens of 8 sequences of 4K to 64K 137 / 85 / 82, 12 tokens of 2 sequences
+// of 32K 61 / 73 / 90.
 struct Cut {
   int rows;  // 32: thin, 64: pair, 128: tile
   int units, pieces, piece;
@@ -1044,7 +1047,8 @@ Cut cut(const lrqk_pages_shape& s) {
     const int64_t want = (int64_t)held * (s.B == 1 ? 1 : c.rows == 32 ? 8 : 2);
     pieces = (want + units - 1) / units;
   } else {
-    // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths
+    // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths (700 tokens at 20K,
+    // 176 tiles of 8 heads: 347 us with 3 pieces, which make 528 workgroups, and 274 with 5)
     pieces = 1;
     double best = 0.0;
     for (int n = 1; n <= 16; ++n) {
@@ -1054,10 +1058,16 @@ Cut cut(const lrqk_pages_shape& s) {
         best = cost;
       }
     }
-    // in a batch there may be sequences of few new tokens and a long context among the others
-    if (s.B > 1) pieces = std::max<int64_t>(pieces, (s.l_max + 32767) / 32768);
+    // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head
+    // would be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not
+    // at the price of partial states of more than a gigabyte.
+    if (s.B > 1) {
+      const int64_t room = (1ll << 30) / ((int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float));
+      pieces = std::max(pieces, std::min<int64_t>((s.l_max + 16383) / 16384, room));
+    }
   }
-  const int64_t piece = std::max<int64_t>((s.l_max + pieces - 1) / pieces, most <= 128 ? 256 : 512);
+  const int64_t least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
+  const int64_t piece = std::max((s.l_max + pieces - 1) / pieces, least);
   c.piece = (int)((piece + 127) / 128 * 128);
   c.pieces = (s.l_max + c.piece - 1) / c.piece;
   c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / rows) times its pieces

@@ -332,6 +332,80 @@ def test_same_call_twice_is_the_same():
             assert torch.equal(c.attend(), c.attend())
 
 
+def exact_on_device(c, b):
+    """What check_attend compares with, for sequence b, in float64 on the GPU: for long contexts."""
+    lo, hi = int(c.start[b]), int(c.start[b + 1])
+    n, Ln = hi - lo, min(int(c.len[b]), c.l_max)
+    p = torch.arange(Ln, device=DEV)
+    pg = c.dtable[b, p // c.page].long()
+    there = (pg >= 0) & (pg < c.n_pages)
+    pg = pg.clamp(0, c.n_pages - 1)
+
+    def rows(name):
+        x = c.d[name][pg, :, p % c.page]
+        if c.sc[name] is None:
+            x = x.double()
+        else:
+            x = x.view(torch.float8_e4m3fn).double() if c.pages == "e4m3" else x.view(torch.int8).double()
+            x = x * torch.exp2(c.ds[name][pg, :, p % c.page].double() - 127).repeat_interleave(32, dim=-1)
+        return torch.where(there[:, None, None], x, 0.0).transpose(0, 1)
+
+    K, V, q = rows("K"), rows("V"), c.q[lo:hi].to(DEV).double()
+    pos = int(c.len[b]) - n + torch.arange(n, device=DEV)
+    hidden = (p[None, :] > pos[:, None]) | ~there[None, :]
+    y, mass, slack = (torch.zeros(n, c.Hq, D, dtype=torch.float64, device=DEV) for _ in range(3))
+    for h in range(c.Hq):
+        k, v = K[h // c.G], V[h // c.G]
+        s = (q[:, h] @ k.t()) * float(np.float32(c.scale))
+        s[hidden] = -float("inf")
+        w = torch.softmax(s, 1)
+        y[:, h], mass[:, h] = w @ v, w @ v.abs()
+        near = torch.where(s >= s.amax(1, keepdim=True) - 100, (q[:, h].abs() @ k.abs().t()) * abs(c.scale) * 130 + 3 * s.abs() + 4, 0.0)
+        slack[:, h] = (2 * near.amax(1) * 2.0 ** -24)[:, None]
+    return y, mass, slack, Ln
+
+
+@pytest.mark.parametrize("kv,pages", KINDS)
+@pytest.mark.parametrize("seqs", [[(300, 20000)], [(1, 70001), (1, 300), (1, 33000)], [(12, 30000), (3, 9000)], [(20, 40000)],
+                                  [(700, 9000), (1, 40000), (2, 17000)]], ids=["chunk", "ones", "pair", "tile", "mixed"])
+def test_long_contexts(seqs, kv, pages):
+    """Many pieces for every shape of workgroup, some of the pages missing."""
+    c = Case(seqs, 2, 4, 64, kv, pages, seed=50, holes=0.05).to_device()
+    out = c.attend().double()
+    for b in range(c.B):
+        y, mass, slack, Ln = exact_on_device(c, b)
+        half = 2.0 ** -8 if kv == "bf16" else 2.0 ** -24
+        tol = half * y.abs() + mass * (slack + 2 * Ln * 2.0 ** -24 + (2.0 ** -8 if kv == "bf16" else 0.0))
+        far = (out[int(c.start[b]):int(c.start[b + 1])] - y).abs() - tol
+        assert float(far.max()) <= 0, f"sequence {b}: off by {float(far.max())} more than the bound"
+
+
+@pytest.mark.parametrize("n,ln", [(1, 3000), (12, 3000), (100, 3000)])
+def test_codes_that_are_no_numbers(n, ln):
+    """A pool from elsewhere may hold the code that e4m3 has for NaN, under an ordinary scale."""
+    c = Case([(n, ln), (1, 70)], 1, 4, 16, "bf16", "e4m3", seed=51)
+    for p, d in ((ln - 1, 7), (ln - max(1, n // 2), 40), (10, 100)):
+        pg, o = c.where(0, p)
+        c.pool["V"][pg, 0, o, d] = 0x7F if p % 2 else 0xFF
+    c.to_device()
+    c.check_attend(c.attend())
+
+
+def test_captured_before_any_call():
+    """A call that is recorded before its kernel has ever run."""
+    c = Case([(1, 333), (2, 40)], 1, 2, 8, "f32", "i8", seed=52).to_device()
+    q, out = c.q.to(DEV), torch.zeros((c.T, c.Hq, D), device=DEV)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L.lrqk_chunk_attend(c.shape, c.pg, q, out, c.ws)
+    for _ in range(3):
+        out.fill_(MARK)
+        g.replay()
+        torch.cuda.synchronize()
+        c.check_attend(out)
+
+
 # ---- rows written and read ---------------------------------------------------------------------------
 def odd_rows(x, pages):
     """Blocks at which a scale or a rounding can go wrong."""
