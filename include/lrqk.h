@@ -521,7 +521,7 @@ int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pages, int3
  * over the positions that exist (their pages too), K and V of KV head h / G.  A token that sees no
  * position, or only scores of -infinity, gets zeros.  What a token does not see does not reach its
  * output, whatever its rows hold.  Products of bf16 operands are exact, sums fp32; with bf16 q the
- * weights are rounded to bf16 before they meet V.
+ * weights are rounded to bf16 before they meet V and before they are summed.
  *   q    device kv_dtype [T,Hq,d]
  *   out  device kv_dtype [T,Hq,d]  written
  *   workspace  device, >= lrqk_pages_workspace_bytes(shape), 256-byte aligned

@@ -9,9 +9,9 @@
 // product takes, as long as it takes the positions in the order in which they lie there (register v, half h:
 // position 8 (v / 4) + 4 h + v % 4), which is how V is read from LDS, four positions at a time through the
 // transposing read.
-// One pass over the positions with a running maximum and sum.  The accumulators are only rescaled when
-// a row's maximum has grown by more than 2^kLag; until then weights up to 2^kLag are kept, which is
-// exact up to the rounding that the weights have anyway.
+// One pass over the positions with a running maximum and sum.  The maximum is raised, and the accumulators
+// rescaled, only when a score exceeds it by more than kLag powers of two (or, in the tiles' steps, when 16 weights exceed
+// kHeavy); until then it is one of an earlier block, which is exact up to the rounding that the weights have anyway.
 //
 // Two shapes of workgroup, both of four wavefronts:
 //   tile  the wavefronts take 32 rows of the problem each and share the positions, 64 at a time (32
@@ -38,6 +38,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.0f;
+constexpr float kHeavy = 4096.0f;
 constexpr int kPartial = kPartialStride;  // floats of a partial state: max, sum, 2 unused, acc[128]
 
 struct Args {
@@ -380,23 +381,20 @@ struct Rows {
     for (int e = 0; e < 16; ++e) s[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? s[e] : -INFINITY;
   }
 
-  static __device__ __forceinline__ float largest(const f32x16& s) {
+  // weights of 32 positions at the running maximum
+  __device__ __forceinline__ f32x16 weigh(const f32x16& s, float c) const {
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    f32x16 w;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base));
+    return w;
+  }
+  // the largest score of the row, in units of log2
+  static __device__ __forceinline__ float largest(const f32x16& s, float c) {
     float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
-    return top;
-  }
-
-  // weights of 32 positions at the running maximum, and their sum
-  __device__ __forceinline__ float weigh(const f32x16& s, float c, f32x16& w) const {
-    const float base = mx == -INFINITY ? 0.0f : mx;
-    float add = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base));
-      add += w[e];
-    }
-    return add;
+    return max_halves(top) * c;
   }
   // the running maximum up to `top`
   __device__ __forceinline__ void raise(float top) {
@@ -421,6 +419,37 @@ struct Rows {
                              dev::pack_bf16(w[8 * k + 4], w[8 * k + 5]), dev::pack_bf16(w[8 * k + 6], w[8 * k + 7]));
     return x;
   }
+  // Their sum, of the weights as they are multiplied, two at a time.
+  static __device__ __forceinline__ float add_up(const Weights& x) {
+    const dev::bf16x2 one = __builtin_bit_cast(dev::bf16x2, 0x3f803f80u);
+    float add = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w[4] = {x.half[k].x, x.half[k].y, x.half[k].z, x.half[k].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        add = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e]), one, add, false);
+    }
+    return add;
+  }
+  static __device__ __forceinline__ float add_up(const f32x16& w) {
+    float add = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) add += w[e];
+    return add;
+  }
+  // the weights of s, at a maximum that is raised where it has to be
+  __device__ __forceinline__ std::conditional_t<BF16, Weights, f32x16> settle(const f32x16& s, float c) {
+    const auto form = [](const f32x16& w) {
+      if constexpr (BF16) return pack(w);
+      else return w;
+    };
+    const float top = largest(s, c);
+    if (__any(top > mx + kLag)) raise(top);  // (-inf > -inf is false: nothing seen so far, nothing to do)
+    const auto x = form(weigh(s, c));
+    sum += add_up(x);
+    return x;
+  }
   // O += weights of 16 positions (half k of 32) times 32 elements (t) of their V rows
   __device__ __forceinline__ void output_step(const char* vt, const Weights& x, int k, int t, int lane) {
     // a transposing read: the 16 lanes of a group point at 4 rows of 16 elements, lane g gets column g
@@ -443,15 +472,6 @@ struct Rows {
       for (int t = 0; t < 4; ++t) output_step(vt, x, k, t, lane);
   }
 
-  // the weights of s, at a maximum that is raised where it has to be
-  __device__ __forceinline__ f32x16 settle(const f32x16& s, float c) {
-    f32x16 w;
-    const float top = max_halves(largest(s)) * c;
-    if (__any(top > mx + kLag)) raise(top);  // (-inf > -inf is false: nothing seen so far, nothing to do)
-    sum += weigh(s, c, w);
-    return w;
-  }
-
   // 32 positions from p0 in LDS, rows `there`; c: scale in log2
   __device__ __forceinline__ void attend(const char* kt, const char* vt, int p0, uint32_t there, bool all_see, float c,
                                          int lane) {
@@ -460,9 +480,9 @@ struct Rows {
       asm volatile("");  // a branch: taken by few blocks
       mask(s, p0, there, lane);
     }
-    const f32x16 w = settle(s, c);
+    const auto w = settle(s, c);
     if constexpr (BF16) {
-      output(vt, pack(w), lane);
+      output(vt, w, lane);
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -480,39 +500,38 @@ struct Rows {
   template <bool BEFORE>
   __device__ __forceinline__ void step(const f32x16& s, f32x16& next, Weights& x, const char* kt, const char* vt, float c,
                                        int lane) {
-    f32x16 w;
     next = zeros();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       next = scores_step(kt, k, next, lane);
       if (BEFORE) output_step(vt, x, k >> 2, k & 3, lane);
     }
-    float add = weigh(s, c, w);
-    const float top = max_halves(largest(s)) * c;
-    x = pack(w);
+    x = pack(weigh(s, c));
+    float add = add_up(x);
     // made here, between the products, and not only once the maximum is known to stand
     asm volatile("" : "+v"(x.half[0].x), "+v"(x.half[0].y), "+v"(x.half[0].z), "+v"(x.half[0].w), "+v"(x.half[1].x),
                       "+v"(x.half[1].y), "+v"(x.half[1].z), "+v"(x.half[1].w), "+v"(add));
-#if 1
+    // reads ahead of the products, then a product, the vector instructions that go under it, a read
     __builtin_amdgcn_sched_group_barrier(0x100, BEFORE ? 6 : 4, 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
       __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, BEFORE ? 2 : 1, 0);
       if (BEFORE) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
         __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
-#endif
-    if (__any(top > mx + kLag)) {
-      raise(top);
-      add = weigh(s, c, w);
-      x = pack(w);
+    // The sum says whether the maximum has to be raised, without the scores being looked through for theirs (eight of some 55
+    // vector instructions).  Where there is no maximum yet the weights may be nothing.
+    if (__any(add > kHeavy || mx == -INFINITY)) {
+      raise(largest(s, c));
+      x = pack(weigh(s, c));
+      add = add_up(x);
     }
     sum += add;
   }
@@ -700,7 +719,7 @@ struct TileLoop {
     if (busy) {
       mask_scores(s, from + t * BN + 32, (uint32_t)(gather_there<16>(there[t & 3]) >> 32));
       r.output(vt, x, lane);
-      x = Rows<true>::pack(r.settle(s, c));
+      x = r.settle(s, c);
       r.output(vt + 32 * kRowB<true>, x, lane);
     }
   }
