@@ -740,49 +740,59 @@ struct PlainLoop {
   uint16_t (*there)[4];
   int half;  // of the block that the wavefront attends to
   B blk;
-  typename B::Found f;
-  typename B::Held hk, hv;
+  struct Way {  // a block on its way: to its buffer in LDS, or, 8-bit, through registers
+    char *k, *v;
+    typename B::Found f;
+    typename B::Held hk, hv;
+  };
 
-  __device__ __forceinline__ void fetch(int p0, char* kt, char* vt, uint16_t* bits) {
+  // (the table entries are asked for before the rows: who waits for them does not wait for these)
+  __device__ __forceinline__ void fetch(int p0, Way& x) {
     const int mine = p0 + w * B::kMine;
-    blk.find(a, p.b, kvh, mine, end, lane, f);
+    blk.find(a, p.b, kvh, mine, end, lane, x.f);
+    blk.look_up(a.m, p.b, mine + BN, end);
     if constexpr (is8(PAGE)) {
-      B::load(a, p.b, kvh, end, a.K, a.K_scale, f, lane, hk);
-      B::load(a, p.b, kvh, end, a.V, a.V_scale, f, lane, hv);
+      B::load(a, p.b, kvh, end, a.K, a.K_scale, x.f, lane, x.hk);
+      B::load(a, p.b, kvh, end, a.V, a.V_scale, x.f, lane, x.hv);
     } else {
-      B::template load_direct<false>(a.K, f, w, lane, kt);
+      B::template load_direct<false>(a.K, x.f, w, lane, x.k);
       const bool part = p0 + BN > least;
-      if (__builtin_expect(f.there == B::kAll && !part, 1)) {
-        B::template load_direct<true>(a.V, f, w, lane, vt);
+      if (__builtin_expect(x.f.there == B::kAll && !part, 1)) {
+        B::template load_direct<true>(a.V, x.f, w, lane, x.v);
       } else {
-        B::load(a, p.b, kvh, end, a.V, nullptr, f, lane, hv);
-        cleared |= B::store_v(hv, f.there, part, w, lane, vt);
+        B::load(a, p.b, kvh, end, a.V, nullptr, x.f, lane, x.hv);
+        cleared |= B::store_v(x.hv, x.f.there, part, w, lane, x.v);
       }
     }
-    if (lane == 0) bits[w] = (uint16_t)f.there;
-    blk.look_up(a.m, p.b, mine + BN, end);
+    if (lane == 0) there[(p0 - from) / BN & 3][w] = (uint16_t)x.f.there;
   }
-  __device__ __forceinline__ void round(int p0, char* kt, char* vt, const uint16_t* bits, char* kt_to, char* vt_to,
-                                        uint16_t* bits_to) {
+  // The block at p0; the next one is on its way, or, with 8-bit rows, the one after the next.
+  __device__ __forceinline__ void round(int p0, Way& now, Way& other) {
     if constexpr (is8(PAGE)) {
-      B::store_k(hk, w, lane, kt);
-      cleared |= B::store_v(hv, f.there, p0 + BN > least, w, lane, vt);
+      B::store_k(now.hk, w, lane, now.k);
+      cleared |= B::store_v(now.hv, now.f.there, p0 + BN > least, w, lane, now.v);
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     __syncthreads();
-    if (p0 + BN < end) fetch(p0 + BN, kt_to, vt_to, bits_to);
+    if constexpr (is8(PAGE)) {
+      if (p0 + 2 * BN < end) fetch(p0 + 2 * BN, now);
+    } else {
+      if (p0 + BN < end) fetch(p0 + BN, other);
+    }
     const int off = 32 * half;
     if (busy)
-      r.attend(kt + off * kRowB<BF16>, vt + off * kRowB<BF16>, p0 + off, (uint32_t)(gather_there<BN / kWaves>(bits) >> off),
-               p0 + off + 32 <= my_least, c, lane);
+      r.attend(now.k + off * kRowB<BF16>, now.v + off * kRowB<BF16>, p0 + off,
+               (uint32_t)(gather_there<BN / kWaves>(there[(p0 - from) / BN & 3]) >> off), p0 + off + 32 <= my_least, c, lane);
   }
   __device__ __forceinline__ void run(char* kt0, char* vt0, char* kt1, char* vt1) {
+    Way x{kt0, vt0, {}, {}, {}}, y{kt1, vt1, {}, {}, {}};
     blk.look_up(a.m, p.b, from + w * B::kMine, end);
-    fetch(from, kt0, vt0, there[0]);
+    fetch(from, x);
+    if (is8(PAGE) && from + BN < end) fetch(from + BN, y);
     for (int p0 = from; p0 < end; p0 += 2 * BN) {
-      round(p0, kt0, vt0, there[0], kt1, vt1, there[1]);
-      if (p0 + BN < end) round(p0 + BN, kt1, vt1, there[1], kt0, vt0, there[0]);
+      round(p0, x, y);
+      if (p0 + BN < end) round(p0 + BN, y, x);
     }
   }
 };
@@ -1046,8 +1056,8 @@ constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 // there are few rows, the context is cut until there are `want` workgroups: as many as the chip holds, and more where a
 // batch's sequences may differ in length, which is not known here.  Measured in us with as many / twice / eight times as
 // many: one token of 16 sequences of 8K to 128K, 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136;
-// pairs, with as many / twice / four times: 5 tokens of 8 sequences of 4K to 64K 137 / 85 / 82, 12 tokens of 2 sequences
-// of 32K 61 / 73 / 90.
+// pairs, with as many / twice / four times: 5 tokens of 8 sequences of 4K to 64K 137 / 76 / 69, 12 tokens of 2 sequences
+// of 32K 61 / 72 / 89.
 struct Cut {
   int rows;  // 32: thin, 64: pair, 128: tile
   int units, pieces, piece;
