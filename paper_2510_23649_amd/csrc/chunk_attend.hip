@@ -13,13 +13,16 @@
 // rescaled, only when a score exceeds it by more than kLag powers of two (or, in the tiles' steps, when 16 weights exceed
 // kHeavy); until then it is one of an earlier block, which is exact up to the rounding that the weights have anyway.
 //
-// Two shapes of workgroup, both of four wavefronts:
+// Three shapes of workgroup, all of four wavefronts:
 //   tile  the wavefronts take 32 rows of the problem each and share the positions, 64 at a time (32
 //         in fp32) through two buffers in LDS: K and V are read once for 128 rows
+//   pair  at most 64 rows (bf16): two wavefronts take 32 rows each at one half of every block of 64
+//         positions, the other two the same rows at the other half
 //   thin  at most 32 rows: each wavefront takes every fourth block of 32 positions through an LDS
-//         area of its own, without a barrier, and the four states are merged at the end
-// Rows are loaded into registers one block ahead (8-bit rows are decoded on the way into LDS, exactly:
-// a code times its scale is a bf16 number).
+//         area of its own, without a barrier
+// The states of wavefronts that have the same rows, and of the pieces that a long context is cut into, are joined at the
+// end.  Rows of the pool's own type go straight to LDS (thin: through registers), 8-bit rows are decoded on the way into
+// it, exactly: a code times its scale is a bf16 number.
 //
 // V rows that a token does not see meet its weights as 0 * V, which is not 0 if V is not finite.
 // Positions that nobody sees are cleared; in blocks that some rows of the problem see and others do not,
@@ -48,12 +51,20 @@ struct Args {
   const void* q;
   void* out;
   float* partials;  // [T*Hq][pieces][kPartial], or null: one piece, straight to out
-  int G, units, pieces, piece;  // units: of a KV head, at most
-  uint32_t page16;  // 16-byte chunks of a page (of all KV heads)
+  int G, pieces, prefer, least;  // pieces: at most, and places in partials; see piece_for
+  uint32_t page16;               // 16-byte chunks of a page (of all KV heads)
   float scale;
 };
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+// Positions of a piece where the longest sequence has that many: a `prefer`th of them, but no more than 16384, and no less
+// than `least` or than there is room for states.
+__host__ __device__ inline int piece_for(int longest, int pieces, int prefer, int least) {
+  const int by_choice = (longest + prefer - 1) / prefer, by_room = (longest + pieces - 1) / pieces;
+  const int p = by_choice < 16384 ? by_choice : 16384;
+  const int q = p > by_room ? p : by_room;
+  return ((q > least ? q : least) + 127) / 128 * 128;
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 using dev::bf16x8;
@@ -62,20 +73,44 @@ using dev::f32x16;
 // Row r of the problem of a sequence: token and query head within the group.
 struct Problem {
   Seq s;
-  int b, piece, r0, rows;  // piece and first row of this workgroup, rows of the sequence
+  int b, step, piece, r0, rows;  // positions of a piece; piece and first row of this workgroup; rows of the sequence
 };
 
-// Unit `unit` of the work of a KV head: a sequence's units are its pieces, last one first, a piece's its tiles (M rows each).  False if there
-// are not that many.  Every wavefront finds it for itself, 64 sequences at a time.
+__device__ __forceinline__ int wave_max(int v) {  // of numbers that are not negative
+  v = max(v, (int)dev::dpp_zero_fill<0x111, 0xf>((uint32_t)v));
+  v = max(v, (int)dev::dpp_zero_fill<0x112, 0xf>((uint32_t)v));
+  v = max(v, (int)dev::dpp_zero_fill<0x114, 0xf>((uint32_t)v));
+  v = max(v, (int)dev::dpp_zero_fill<0x118, 0xf>((uint32_t)v));
+  v = max(v, (int)dev::dpp_zero_fill<0x142, 0xa>((uint32_t)v));
+  v = max(v, (int)dev::dpp_zero_fill<0x143, 0xc>((uint32_t)v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Positions of a piece in this call: the lengths say, not l_max, which a captured call has for all its replays.  The whole
+// wavefront asks.
+__device__ __forceinline__ int piece_of(const Args& a, int first_len) {
+  const int lane = threadIdx.x & 63;
+  int longest = first_len;
+  for (int i0 = 64; i0 < a.m.B; i0 += 64) longest = max(longest, a.m.kv_len[min(i0 + lane, a.m.B - 1)]);
+  return piece_for(wave_max(min(max(longest, 0), a.m.l_max)), a.pieces, a.prefer, a.least);
+}
+// kv_len of sequence `lane`, which piece_of starts from
+__device__ __forceinline__ int first_len(const Args& a) { return a.m.kv_len[min((int)(threadIdx.x & 63), a.m.B - 1)]; }
+
+// Unit `unit` of the work of a KV head: a sequence's units are its pieces, last one first, a piece's its tiles (M rows
+// each).  False if there are not that many.  Every wavefront finds it for itself, 64 sequences at a time.
 template <int M>
 __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
   const int lane = threadIdx.x & 63;
+  const int len0 = first_len(a);
+  p.step = 0;
   int before = 0;
   for (int i0 = 0; i0 < a.m.B; i0 += 64) {
     const int i = min(i0 + lane, a.m.B - 1);
-    const int len = max(a.m.kv_len[i], 0);  // with the starts, not after them
+    const int len = max(i0 == 0 ? len0 : a.m.kv_len[i], 0);  // with the starts, not after them
     const int first = min(max(a.m.start[i], 0), a.m.T), n = min(max(a.m.start[i + 1], first), a.m.T) - first;
-    const int tiles = (n * a.G + M - 1) / M, pieces = max(1, (min(len, a.m.l_max) + a.piece - 1) / a.piece);
+    if (i0 == 0) p.step = piece_of(a, len0);
+    const int tiles = (n * a.G + M - 1) / M, pieces = max(1, (min(len, a.m.l_max) + p.step - 1) / p.step);
     const int units = i0 + lane < a.m.B ? tiles * pieces : 0;
     const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)units);
     const uint64_t past = __ballot(upto > unit);
@@ -607,7 +642,7 @@ __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows,
 template <int BITS>
 __device__ __forceinline__ uint64_t gather_there(const uint16_t* there) {
   uint64_t x;
-  if constexpr (BITS == 16) x = *reinterpret_cast<const uint64_t*>(there);
+  if constexpr (BITS == 16) __builtin_memcpy(&x, there, 8);
   else x = there[0] | there[1] << 8 | there[2] << 16 | (uint64_t)there[3] << 24;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
   return (uint64_t)hi << 32 | lo;
@@ -810,7 +845,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = min(M, p.rows - p.r0);
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-  const int from = p.piece * a.piece, end = min(most, from + a.piece);
+  const int from = p.piece * p.step, end = min(most, from + p.step);
   if (from >= end && p.piece > 0) return;  // (piece 0 writes the rows that see nothing)
   const int mine = p.r0 + w * 32 + (lane & 31), last = p.rows - 1;  // rows behind the last repeat it
   Rows<BF16> r;
@@ -890,7 +925,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
     if (!find_unit<M>(a, unit, p)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-    const int from = p.piece * a.piece, end = min(most, from + a.piece);
+    const int from = p.piece * p.step, end = min(most, from + p.step);
     if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
     Rows<BF16> r;
     const int real = min(p.r0 + (lane & 31), p.rows - 1);
@@ -948,7 +983,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) 
     if (!find_unit<M>(a, unit, p)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
-    const int from = p.piece * a.piece, end = min(most, from + a.piece);
+    const int from = p.piece * p.step, end = min(most, from + p.step);
     if (from >= end && p.piece > 0) continue;
     Rows<true> r;
     const int real = min(p.r0 + 32 * set + (lane & 31), p.rows - 1);
@@ -978,6 +1013,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   const int64_t at = (int64_t)blockIdx.x * (kWaves / W) + wave / W;
   const int Hq = a.m.Hkv * a.G;
   const int t = (int)min(at / Hq, (int64_t)a.m.T);
+  const int step = piece_of(a, first_len(a));
   const int b = sequence_of(a.m, t);
   bool mine = at < n_rows && b >= 0;
   int pieces = 0;
@@ -985,7 +1021,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
     const Seq s = sequence(a.m, b);
     mine = t >= s.first && t < s.first + s.n;
     const int see = min(max(s.len - s.n + (t - s.first) + 1, 0), a.m.l_max);
-    pieces = max(1, (see + a.piece - 1) / a.piece);
+    pieces = max(1, (see + step - 1) / step);
   }
   if (W == 1 && !mine) return;
   float mx = -INFINITY, sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
@@ -1060,7 +1096,7 @@ constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 // of 32K 61 / 72 / 89.
 struct Cut {
   int rows;  // 32: thin, 64: pair, 128: tile
-  int units, pieces, piece;
+  int units, pieces, prefer, least;  // units: of a KV head, at most; the others: piece_for
 };
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
@@ -1087,18 +1123,18 @@ Cut cut(const lrqk_pages_shape& s) {
         best = cost;
       }
     }
-    // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head
-    // would be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not
-    // at the price of partial states of more than a gigabyte.
-    if (s.B > 1) {
-      const int64_t room = (1ll << 30) / ((int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float));
-      pieces = std::max(pieces, std::min<int64_t>((s.l_max + 16383) / 16384, room));
-    }
   }
-  const int64_t least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
-  const int64_t piece = std::max((s.l_max + pieces - 1) / pieces, least);
-  c.piece = (int)((piece + 127) / 128 * 128);
-  c.pieces = (s.l_max + c.piece - 1) / c.piece;
+  c.least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
+  c.prefer = (int)std::min<int64_t>(pieces, (s.l_max + c.least - 1) / c.least);
+  // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head would
+  // be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not at the
+  // price of partial states of more than a gigabyte.
+  c.pieces = c.prefer;
+  if (s.B > 1) {
+    const int64_t room = (1ll << 30) / ((int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float));
+    c.pieces = (int)std::max<int64_t>(c.pieces, std::min<int64_t>((s.l_max + 16383) / 16384, room));
+  }
+  if (c.pieces == 1) c.least = s.l_max;
   c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / rows) times its pieces
   return c;
 }
@@ -1162,7 +1198,7 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   if (ws_bytes < lrqk_pages_workspace_bytes(shape)) return LRQK_ENOMEM;
   const Cut c = cut(s);
   const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
-               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.units, c.pieces, c.piece,
+               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.pieces, c.prefer, c.least,
                (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(kD * page_elem_bytes(s.page_dtype) / 16), s.scale};
   hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {

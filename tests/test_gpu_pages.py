@@ -288,6 +288,14 @@ def test_n_max_only_chooses_the_kernel():
             c.check_attend(c.attend())
 
 
+@pytest.mark.parametrize("seqs", [[(1, 700), (1, 90)], [(12, 1300), (2, 40)], [(60, 700), (1, 300)]], ids=["ones", "pair", "tile"])
+def test_l_max_far_above_the_lengths(seqs):
+    """A call may be made for contexts much longer than those that there are."""
+    for l_max in (2000, 131072, 3000001):
+        c = Case(seqs, 2, 4, 64, "bf16", "bf16", seed=17, l_max=l_max).to_device()
+        c.check_attend(c.attend())
+
+
 def test_many_sequences():
     """More sequences than a wavefront has lanes."""
     rng = np.random.default_rng(14)
