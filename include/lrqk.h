@@ -441,11 +441,13 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  * p mod page of page table[b][p / page].
  *   - A table entry outside [0, n_pages) is no page: rows written to it are dropped, rows read from it
  *     are left alone in the output, positions on it take no part in an attention.  Several
- *     sequences may share a page (a common prefix); a row that two calls, or two sequences of a
- *     call, write holds what either wrote.
+ *     sequences may share a page (a common prefix).  A row that is written twice at a time (by two
+ *     sequences of a call, by two entries of a table with the same page, by calls that overlap) holds
+ *     parts of either, in 8 bits perhaps the codes of one under the scales of the other: it is only
+ *     good if both write the same.
  *   - Positions below 0 or from l_max on do not exist (the same rules).
- *   - Rows of the packed arrays before start[0] and from start[B] on belong to no sequence: not read,
- *     and left as they were in outputs.
+ *   - Rows of the packed arrays before start[0] and from start[B] on belong to no sequence: what
+ *     they hold does not matter, and in outputs they stay as they were.
  *   - Rows of a page that no position reaches may hold anything, infinities and NaN included.
  * start, kv_len and table are device memory and are read by the kernels only: a captured call follows
  * what they hold when it is replayed.

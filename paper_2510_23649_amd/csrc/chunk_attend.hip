@@ -176,7 +176,7 @@ __device__ __forceinline__ int k_chunk(int row, int c) {
 }
 __device__ __forceinline__ int v_turn(int row) { return ((row & 3) << 2) ^ (((row >> 2) & 1) << 1); }
 __device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true> + ((c ^ v_turn(row)) << 4); }
-//
+
 // Blocks and a wavefront's share of them begin at multiples of 16 positions (8 in fp32), so with pages of 16 positions
 // and more up to 16 rows at a time lie one behind the other in one page: their place is one number for the wavefront,
 // and a lane's part of an address does not change from block to block.  SMALL: smaller pages, a table entry for every row.
