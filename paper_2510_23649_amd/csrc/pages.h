@@ -58,7 +58,8 @@ __device__ __forceinline__ int64_t row_of(const Map& m, int b, int kvh, int p) {
 
 // 2^(byte - 127); 255: NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
+  const uint32_t x = max(byte << 23, 0x00400000u);
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : x);
 }
 
 // Eight codes (two dwords) times their scale, in fp32 (exact).
