@@ -835,6 +835,14 @@ struct PlainLoop {
   }
 };
 
+// 128 rows of the problem, 32 a wavefront.  Bound by the matrix cores and the vector instructions between their products: a
+// step of 32 positions has 16 products (32 cycles each) and some 65 vector instructions, and two wavefronts a SIMD are what
+// the registers allow.  2048 tokens at 32K, bf16, 32 + 8 heads: 1030 us, 1.03 PFLOP/s, matrix cores busy 44% of the cycles, no
+// LDS bank conflict; 8-bit rows are decoded once a workgroup, between the rounds (1024 tokens at 128K of e4m3: 2450 us,
+// 0.89 PFLOP/s).  64 rows a wavefront, one a SIMD, halve the decoding and the reads of LDS and took longer (1160 and 3007 us
+// where this took 1030 and 2560): what a wavefront waits for is then not covered by another one's products.  Decoding between a
+// step's products does not fit the registers (90 spilled).  fp32: 1001 tokens at 5003 and 744 at 1315, 660 us with the join, 113 TFLOP/s; 2048 tokens at 16K
+// 133 TFLOP/s of the 153 that a matrix product reaches.
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
   using Loop = std::conditional_t<BF16, TileLoop<PAGE>, PlainLoop<false, PAGE, 32>>;
@@ -912,6 +920,10 @@ __device__ __forceinline__ void leave_state(const Rows<BF16>& r, int at, int lan
   }
 }
 
+// At most 32 rows a workgroup: K and V are read once and the matrix cores wait, so this is bound by memory where there is
+// enough of it to read, and by the latency of loads that depend on each other where there is little.  No barrier between a
+// wavefront's blocks, the next one in registers on its way.  One token of 16 sequences of 8K to 128K, e4m3, 2.1 GB: 383 us with
+// the join, 5.6 TB/s; one token at 4K, bf16: 13 us, 8 of them here and 4 in the join.
 template <bool BF16, int PAGE, bool SMALL>
 __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(const Args a) {
   constexpr int M = 32, BN = 32;
@@ -970,6 +982,9 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   }
 }
 
+// 33 to 64 rows: rows of the pool are read and decoded once for all of them, which a thin workgroup per 32 rows would do
+// twice.  Bound by the decoding and the barriers between blocks more than by memory.  1 to 5 tokens of 8 sequences of 7K to 64K,
+// 7 heads a group, i8, 192 MB: 75 us with the join, 2.6 TB/s; as thin workgroups with two sets of rows a wavefront 101 us.
 template <int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) {
   using Loop = PlainLoop<true, PAGE, 64>;
@@ -1008,7 +1023,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) 
 }
 
 // The pieces of a row's context joined: W wavefronts a row, each takes its share of the pieces, a piece's maximum and sum
-// in a lane, two elements a lane.  All loads of a share are independent of each other.
+// in a lane, two elements a lane.  All loads of a share are independent of each other: bound by latency, 4 us of the 13 of one
+// token at 4K (32 pieces), 8 of 383 at 16 sequences of up to 128K.
 template <bool BF16, int W>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int64_t n_rows) {
   __shared__ float part[kWaves][2 + kD];

