@@ -51,19 +51,11 @@ struct Args {
   const void* q;
   void* out;
   float* partials;  // [T*Hq][pieces][kPartial], or null: one piece, straight to out
-  int G, pieces, prefer, least;  // pieces: at most, and places in partials; see piece_for
+  int G, rows_log2;                    // rows of the problem a workgroup takes
+  int pieces, prefer, want, least;     // pieces: of a sequence at most, and places in partials; see piece_of
   uint32_t page16;               // 16-byte chunks of a page (of all KV heads)
   float scale;
 };
-
-// Positions of a piece where the longest sequence has that many: a `prefer`th of them, but no more than 16384, and no less
-// than `least` or than there is room for states.
-__host__ __device__ inline int piece_for(int longest, int pieces, int prefer, int least) {
-  const int by_choice = (longest + prefer - 1) / prefer, by_room = (longest + pieces - 1) / pieces;
-  const int p = by_choice < 16384 ? by_choice : 16384;
-  const int q = p > by_room ? p : by_room;
-  return ((q > least ? q : least) + 127) / 128 * 128;
-}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -86,31 +78,82 @@ __device__ __forceinline__ int wave_max(int v) {  // of numbers that are not neg
   return __builtin_amdgcn_readlane(v, 63);
 }
 
-// Positions of a piece in this call: the lengths say, not l_max, which a captured call has for all its replays.  The whole
-// wavefront asks.
-__device__ __forceinline__ int piece_of(const Args& a, int first_len) {
-  const int lane = threadIdx.x & 63;
-  int longest = first_len;
-  for (int i0 = 64; i0 < a.m.B; i0 += 64) longest = max(longest, a.m.kv_len[min(i0 + lane, a.m.B - 1)]);
-  return piece_for(wave_max(min(max(longest, 0), a.m.l_max)), a.pieces, a.prefer, a.least);
+// Sequence i0 + lane (behind the last one: that again).
+__device__ __forceinline__ Seq lane_sequence(const Args& a, int i0) {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // (addresses made anew, and not kept in registers over all units)
+  const int i = min(i0 + lane, a.m.B - 1);
+  const int len = a.m.kv_len[i], first = a.m.start[i], end = a.m.start[i + 1];  // together, not one after the other
+  Seq s;
+  s.first = min(max(first, 0), a.m.T);
+  s.n = min(max(end, s.first), a.m.T) - s.first;
+  s.len = max(len, 0);
+  return s;
 }
-// kv_len of sequence `lane`, which piece_of starts from
-__device__ __forceinline__ int first_len(const Args& a) { return a.m.kv_len[min((int)(threadIdx.x & 63), a.m.B - 1)]; }
+__device__ __forceinline__ int tiles_of(const Args& a, int n) { return (n * a.G + (1 << a.rows_log2) - 1) >> a.rows_log2; }
+
+// The same in all lanes: of numbers that are not negative.
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  return __builtin_amdgcn_readlane(dev::wave_inclusive_scan(v), 63);
+}
+
+// Positions of a piece in this call: the lengths say, not l_max, which a captured call has for all its replays.  The whole
+// wavefront asks, with the first 64 sequences.
+//   want > 0   few rows a sequence: as short as it can be without there being more than `want` units of work a KV head.  With
+//              t_b tiles of sequence b, t = sum_b t_b and x = sum_b t_b len_b, at least x / want, and surely enough x / (want - t + 1),
+//              as sum_b t_b ceil(len_b / p) <= ceil(x / p) + t - 1; up to 64 sequences' units are counted for some between
+//   want == 0  many: a `prefer`th of the longest sequence, but no more than 16384
+// and no less than `least` or than there is room for states.  EVEN: want may be > 0.
+template <bool EVEN>
+__device__ __forceinline__ int piece_of(const Args& a, Seq s) {
+  const int lane = threadIdx.x & 63;
+  int longest = 0, p;
+  if (EVEN && a.want > 0) {
+    uint32_t x = 0, t = 0, len, mine;  // lengths in 128 positions; 32 bits hold x: want > 0 only if B <= 4096
+    for (int i0 = 0;;) {
+      mine = i0 + lane < a.m.B ? (uint32_t)tiles_of(a, s.n) : 0;
+      len = mine > 0 ? ((uint32_t)min(s.len, a.m.l_max) + 127) >> 7 : 0;
+      longest = max(longest, (int)len);
+      x += mine * len;
+      t += mine;
+      i0 += 64;
+      if (i0 >= a.m.B) break;
+      s = lane_sequence(a, i0);
+    }
+    longest = wave_max(longest) * 128;
+    x = wave_sum(x);
+    t = wave_sum(t);
+    const uint32_t parts = (uint32_t)max(a.want - (int)t + 1, 1), enough = (x + parts - 1) / parts;
+    uint32_t q = (x + a.want - 1) / a.want;
+    const uint32_t by = (enough - q + 3) / 4;
+    if (a.m.B > 64) q = enough;
+    while (q < enough && wave_sum(mine * max((len + q - 1) / q, 1u)) > (uint32_t)a.want) q = min(q + by, enough);
+    p = (int)q * 128;
+  } else {
+    for (int i0 = 0;;) {
+      longest = max(longest, min(s.len, a.m.l_max));
+      i0 += 64;
+      if (i0 >= a.m.B) break;
+      s = lane_sequence(a, i0);
+    }
+    longest = wave_max(longest);
+    p = min((longest + a.prefer - 1) / a.prefer, 16384);
+  }
+  p = max(max(p, (longest + a.pieces - 1) / a.pieces), a.least);
+  return (p + 127) / 128 * 128;
+}
 
 // Unit `unit` of the work of a KV head: a sequence's units are its pieces, last one first, a piece's its tiles (M rows
 // each).  False if there are not that many.  Every wavefront finds it for itself, 64 sequences at a time.
-template <int M>
+template <int M, bool EVEN>
 __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
   const int lane = threadIdx.x & 63;
-  const int len0 = first_len(a);
-  p.step = 0;
+  Seq q = lane_sequence(a, 0);
+  p.step = piece_of<EVEN>(a, q);
   int before = 0;
   for (int i0 = 0; i0 < a.m.B; i0 += 64) {
-    const int i = min(i0 + lane, a.m.B - 1);
-    const int len = max(i0 == 0 ? len0 : a.m.kv_len[i], 0);  // with the starts, not after them
-    const int first = min(max(a.m.start[i], 0), a.m.T), n = min(max(a.m.start[i + 1], first), a.m.T) - first;
-    if (i0 == 0) p.step = piece_of(a, len0);
-    const int tiles = (n * a.G + M - 1) / M, pieces = max(1, (min(len, a.m.l_max) + p.step - 1) / p.step);
+    if (i0 > 0) q = lane_sequence(a, i0);
+    const int tiles = (q.n * a.G + M - 1) / M, pieces = max(1, (min(q.len, a.m.l_max) + p.step - 1) / p.step);
     const int units = i0 + lane < a.m.B ? tiles * pieces : 0;
     const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)units);
     const uint64_t past = __ballot(upto > unit);
@@ -119,9 +162,9 @@ __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
       const int mine = unit - (__builtin_amdgcn_readlane(upto, j) - __builtin_amdgcn_readlane(units, j));
       const int t = __builtin_amdgcn_readlane(tiles, j);
       p.b = i0 + j;
-      p.s.first = __builtin_amdgcn_readlane(first, j);
-      p.s.n = __builtin_amdgcn_readlane(n, j);
-      p.s.len = __builtin_amdgcn_readlane(len, j);
+      p.s.first = __builtin_amdgcn_readlane(q.first, j);
+      p.s.n = __builtin_amdgcn_readlane(q.n, j);
+      p.s.len = __builtin_amdgcn_readlane(q.len, j);
       p.rows = p.s.n * a.G;
       if (mine < 0) return false;  // (no start may send a workgroup anywhere)
       // the last tiles of a sequence see most: they come first
@@ -852,7 +895,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   // KV head fastest: the dies take workgroups in turn, so a head's rows stay in one die's L2
   const int kvh = blockIdx.x % a.m.Hkv;
   Problem p;
-  if (!find_unit<M>(a, blockIdx.x / a.m.Hkv, p)) return;
+  if (!find_unit<M, true>(a, blockIdx.x / a.m.Hkv, p)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = min(M, p.rows - p.r0);
   const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
@@ -937,7 +980,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
     Problem p;
-    if (!find_unit<M>(a, unit, p)) return;
+    if (!find_unit<M, !BF16>(a, unit, p)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
     const int from = p.piece * p.step, end = min(most, from + p.step);
@@ -984,7 +1027,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
 
 // 33 to 64 rows: rows of the pool are read and decoded once for all of them, which a thin workgroup per 32 rows would do
 // twice.  Bound by the decoding and the barriers between blocks more than by memory.  1 to 5 tokens of 8 sequences of 7K to 64K,
-// 7 heads a group, i8, 192 MB: 75 us with the join, 2.6 TB/s; as thin workgroups with two sets of rows a wavefront 101 us.
+// 7 heads a group, i8, 192 MB: 63 us with the join, 3.0 TB/s (75 with pieces from the longest sequence alone: no more than 372 of the 512
+// workgroups had any; as thin workgroups with two sets of rows a wavefront 101).
 template <int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) {
   using Loop = PlainLoop<true, PAGE, 64>;
@@ -998,7 +1042,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) 
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // (as above)
     Problem p;
-    if (!find_unit<M>(a, unit, p)) return;
+    if (!find_unit<M, true>(a, unit, p)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
     const int from = p.piece * p.step, end = min(most, from + p.step);
@@ -1032,7 +1076,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   const int64_t at = (int64_t)blockIdx.x * (kWaves / W) + wave / W;
   const int Hq = a.m.Hkv * a.G;
   const int t = (int)min(at / Hq, (int64_t)a.m.T);
-  const int step = piece_of(a, first_len(a));
+  const int step = piece_of<true>(a, lane_sequence(a, 0));
   const int b = sequence_of(a.m, t);
   bool mine = at < n_rows && b >= 0;
   int pieces = 0;
@@ -1107,54 +1151,60 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
 // How a call is cut up.  At most 32 rows a sequence and KV head go the thin way, and all calls with pages of less than 16
-// positions; up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit); more in tiles.  Where
-// there are few rows, the context is cut until there are `want` workgroups: as many as the chip holds, and more where a
-// batch's sequences may differ in length, which is not known here.  Measured in us with as many / twice / eight times as
-// many: one token of 16 sequences of 8K to 128K, 8-bit rows, 512 / 427 / 384; of one sequence of 128K 103 / 110 / 136;
-// pairs, with as many / twice / four times: 5 tokens of 8 sequences of 4K to 64K 137 / 76 / 69, 12 tokens of 2 sequences
-// of 32K 61 / 72 / 89.
+// positions; up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit); more in tiles.
 struct Cut {
   int rows;  // 32: thin, 64: pair, 128: tile
-  int units, pieces, prefer, least;  // units: of a KV head, at most; the others: piece_for
+  int units, pieces, prefer, want, least;  // units: of a KV head, at most; the others: piece_of
 };
 Cut cut(const lrqk_pages_shape& s) {
   const int G = s.Hq / s.Hkv;
   const int64_t most = (int64_t)s.n_max * G;
+  const bool f32 = s.kv_dtype == LRQK_KV_F32;
   Cut c;
-  c.rows = most <= 32 || s.page < 16 ? 32 : most <= 64 && s.kv_dtype == LRQK_KV_BF16 ? 64 : 128;
-  const int tiles = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows);
-  const int64_t units = (int64_t)std::max(s.B, tiles) * s.Hkv;
+  c.rows = most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
+  const int full = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows), tiles = full + s.B;  // sum_b ceil(n_b G / rows) is no more
+  const int64_t units = (int64_t)std::max(s.B, full) * s.Hkv;
   // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
-  const int held = c.rows == 32 && s.kv_dtype == LRQK_KV_F32 ? 256 : 512;
-  int64_t pieces;
-  if (most <= 128) {
-    const int64_t want = (int64_t)held * (s.B == 1 ? 1 : c.rows == 32 ? 8 : 2);
-    pieces = (want + units - 1) / units;
-  } else {
-    // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths (700 tokens at 20K,
-    // 176 tiles of 8 heads: 347 us with 3 pieces, which make 528 workgroups, and 274 with 5)
-    pieces = 1;
-    double best = 0.0;
-    for (int n = 1; n <= 16; ++n) {
-      const double cost = (double)((units * n + held - 1) / held) / n * (1.0 + 0.04 * (n - 1));
-      if (n == 1 || cost < best) {
-        pieces = n;
-        best = cost;
-      }
-    }
-  }
-  c.least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
-  c.prefer = (int)std::min<int64_t>(pieces, (s.l_max + c.least - 1) / c.least);
+  const int held = c.rows == 32 && f32 ? 256 : 512;
+  const int64_t state = (int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float);
   // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head would
   // be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not at the
   // price of partial states of more than a gigabyte.
-  c.pieces = c.prefer;
-  if (s.B > 1) {
-    const int64_t room = (1ll << 30) / ((int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float));
-    c.pieces = (int)std::max<int64_t>(c.pieces, std::min<int64_t>((s.l_max + 16383) / 16384, room));
+  const int64_t few = s.B > 1 ? std::min<int64_t>((s.l_max + 16383) / 16384, (1ll << 30) / state) : 1;
+  c.least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
+  const int64_t least = (s.l_max + c.least - 1) / c.least;  // pieces, with those
+  c.prefer = 1;
+  c.want = 0;
+  if (most <= 128 && s.B <= 4096 && (c.rows != 32 || f32)) {
+    // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
+    // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 63 / 70 / 78; 12 tokens of 2 sequences of 32K
+    // 62 / 74 / 85; fp32, one token of 4 sequences of 32K 225 / 226, and 249 with four times as many.  States of 64 MiB at most.
+    c.want = std::max((held + s.Hkv - 1) / s.Hkv, 2 * tiles);
+    c.pieces = (int)std::max(few, std::min<int64_t>({c.want, least, std::max<int64_t>((1ll << 26) / state, 1)}));
+    c.units = c.want;
+  } else {
+    if (most <= 128) {
+      // Bound by memory where a batch has enough of it: more units than the chip holds, so that all of it reads to the end.
+      // With as many / twice / eight times as many: one token of 16 sequences of 8K to 128K, 8-bit rows, 512 / 427 / 384; of
+      // one sequence of 128K 103 / 110 / 136.
+      c.prefer = (int)std::min<int64_t>(((int64_t)held * (s.B == 1 ? 1 : 8) + units - 1) / units, least);
+    } else {
+      // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths (700 tokens at 20K,
+      // 176 tiles of 8 heads: 347 us with 3 pieces, which make 528 workgroups, and 274 with 5)
+      double best = 0.0;
+      for (int n = 1; n <= 16; ++n) {
+        const double cost = (double)((units * n + held - 1) / held) / n * (1.0 + 0.04 * (n - 1));
+        if (n == 1 || cost < best) {
+          c.prefer = n;
+          best = cost;
+        }
+      }
+      c.prefer = (int)std::min<int64_t>(c.prefer, least);
+    }
+    c.pieces = (int)std::max<int64_t>(c.prefer, few);
+    c.units = tiles * c.pieces;
   }
   if (c.pieces == 1) c.least = s.l_max;
-  c.units = (tiles + s.B) * c.pieces;  // no fewer than sum_b ceil(n_b G / rows) times its pieces
   return c;
 }
 size_t partial_bytes(const lrqk_pages_shape& s) {
@@ -1217,7 +1267,8 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   if (ws_bytes < lrqk_pages_workspace_bytes(shape)) return LRQK_ENOMEM;
   const Cut c = cut(s);
   const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
-               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv, c.pieces, c.prefer, c.least,
+               c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv,
+               __builtin_ctz((unsigned)c.rows), c.pieces, c.prefer, c.want, c.least,
                (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(kD * page_elem_bytes(s.page_dtype) / 16), s.scale};
   hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {

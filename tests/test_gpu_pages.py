@@ -303,6 +303,16 @@ def test_many_sequences():
     c.check_attend(c.attend())
 
 
+@pytest.mark.parametrize("B", [2, 64, 65, 150])
+@pytest.mark.parametrize("n,kv", [(12, "bf16"), (25, "bf16"), (3, "f32"), (20, "f32")], ids=["pair", "tile", "thin_f32", "tile_f32"])
+def test_uneven_batches(n, kv, B):
+    """One long sequence among short ones, empty ones and ones without new tokens: their pieces, up to 64 sequences and beyond."""
+    rng = np.random.default_rng(B)
+    seqs = [(int(rng.integers(0, n + 1)), int(rng.integers(0, 200))) for _ in range(B - 1)] + [(n, 9000)]
+    c = Case([seqs[i] for i in rng.permutation(B)], 1, 4, 16, kv, kv, seed=15, n_max=n).to_device()
+    c.check_attend(c.attend())
+
+
 @pytest.mark.parametrize("pages", ["e4m3", "bf16"])
 def test_offsets_beyond_32_bits(pages):
     """A pool of more than 2^32 elements, its last pages in use."""
