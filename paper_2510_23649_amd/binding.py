@@ -388,7 +388,7 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
 
 def _fits(t: Optional[torch.Tensor], shape: PagesShape, rows: int, pinned=False):
     """Pointer of a contiguous tensor of shape.kv_dtype with at least `rows` rows of d elements, on
-    the current device (or, with `pinned`, in pinned host memory)."""
+    a device (or, with `pinned`, in pinned host memory)."""
     if t is None:
         return None
     want = torch.bfloat16 if shape.kv_dtype == LRQK_KV_BF16 else torch.float32
@@ -398,27 +398,26 @@ def _fits(t: Optional[torch.Tensor], shape: PagesShape, rows: int, pinned=False)
         raise ValueError(f"expected {rows} rows of {shape.d}, got {tuple(t.shape)}")
     if pinned and not t.is_cuda:
         return _pinned(t)
-    ptr = _dev(t)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensor on {t.device}, current device is {torch.cuda.current_device()}")
-    return ptr
+    return _dev(t)
 
 
-def _raw_stream(stream, pages: Pages) -> Optional[int]:
-    """As _stream, for a call on `pages`; the current one without the object around it (3 us of a call of 9)."""
-    device = getattr(pages, "device", None)
-    if device is not None and device != torch.cuda.current_device():
-        raise ValueError(f"pages on device {device}, current device is {torch.cuda.current_device()}")
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    return _stream(stream)
+def _raw_stream(stream, pages: Pages, *tensors) -> Optional[int]:
+    """As _stream, for a call on `pages` and `tensors`, which have to be on the current device (or on
+    the host); the current stream without the object around it (3 us of a call of 9)."""
+    here = torch.cuda.current_device()
+    if getattr(pages, "device", here) != here:
+        raise ValueError(f"pages on device {pages.device}, current device is {here}")
+    for t in tensors:
+        if t is not None and t.get_device() not in (here, -1):
+            raise ValueError(f"tensor on {t.device}, current device is {here}")
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
 
 
 def lrqk_pages_append(shape, pages, k_new, v_new, stream=None):
     rows = shape.T * shape.Hkv
     _check(load_library().lrqk_pages_append(C.byref(shape), C.byref(pages),
                                             _fits(k_new, shape, rows), _fits(v_new, shape, rows),
-                                            _raw_stream(stream, pages)), "lrqk_pages_append")
+                                            _raw_stream(stream, pages, k_new, v_new)), "lrqk_pages_append")
 
 
 def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
@@ -426,7 +425,7 @@ def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
     _check(load_library().lrqk_pages_read(C.byref(shape), C.byref(pages), int(first),
                                           _fits(K_out, shape, rows, pinned=True),
                                           _fits(V_out, shape, rows, pinned=True),
-                                          _raw_stream(stream, pages)), "lrqk_pages_read")
+                                          _raw_stream(stream, pages, K_out, V_out)), "lrqk_pages_read")
 
 
 def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
@@ -435,5 +434,5 @@ def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
         raise ValueError(f"workspace on {workspace.device}, out on {out.device}")
     _check(load_library().lrqk_chunk_attend(
         C.byref(shape), C.byref(pages), _fits(q, shape, rows), _fits(out, shape, rows),
-        _dev(workspace), workspace.numel() * workspace.element_size(), _raw_stream(stream, pages)),
+        _dev(workspace), workspace.numel() * workspace.element_size(), _raw_stream(stream, pages, q, out)),
         "lrqk_chunk_attend")
