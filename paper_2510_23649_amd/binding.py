@@ -383,7 +383,37 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
     p.device = K.device.index
     if any(t is not None and t.device.index != p.device for t in p.tensors):
         raise ValueError("pages on several devices")
+    p.fits = None
     return p
+
+
+_PAGE_ROWS = {LRQK_PAGE_BF16: (torch.bfloat16,), LRQK_PAGE_F32: (torch.float32,)}
+
+
+def _hold(pages: Pages, shape: PagesShape):
+    """The tensors of make_pages have the types that `shape` says and at least its sizes: a kernel reaches
+    nothing beside them.  What a shape was found to fit is not looked at again until another one comes (0.2 us
+    of a call, 3 if it is looked at).  Pages made from raw pointers are the caller's."""
+    key = bytes(shape)
+    if getattr(pages, "tensors", None) is None or pages.fits == key:
+        return
+    if lrqk_validate_pages(shape) != 0:
+        return                               # the call says so
+    K, V, K_scale, V_scale, table, start, kv_len = pages.tensors
+    eight = _PAGE_TYPES - {torch.bfloat16, torch.float32}
+    if K.dtype not in _PAGE_ROWS.get(shape.page_dtype, eight):
+        raise TypeError(f"pages of {K.dtype}, page_dtype {shape.page_dtype}")
+    rows = shape.n_pages * shape.Hkv * shape.page
+    need = [("K", K, rows * shape.d), ("V", V, rows * shape.d), ("table", table, shape.B * shape.max_pages),
+            ("start", start, shape.B + 1), ("kv_len", kv_len, shape.B)]
+    if shape.page_dtype not in _PAGE_ROWS:
+        need += [("K_scale", K_scale, rows * (shape.d // 32)), ("V_scale", V_scale, rows * (shape.d // 32))]
+    for name, t, n in need:
+        if t is not None and t.numel() < n:  # (missing scales: the call says so)
+            raise ValueError(f"{name}: expected {n} elements, got {tuple(t.shape)}")
+    if shape.B > 1 and table.dim() == 2 and table.shape[1] != shape.max_pages:
+        raise ValueError(f"table rows of {table.shape[1]} entries, max_pages {shape.max_pages}")
+    pages.fits = key
 
 
 def _fits(t: Optional[torch.Tensor], shape: PagesShape, rows: int, pinned=False):
@@ -414,6 +444,7 @@ def _raw_stream(stream, pages: Pages, *tensors) -> Optional[int]:
 
 
 def lrqk_pages_append(shape, pages, k_new, v_new, stream=None):
+    _hold(pages, shape)
     rows = shape.T * shape.Hkv
     _check(load_library().lrqk_pages_append(C.byref(shape), C.byref(pages),
                                             _fits(k_new, shape, rows), _fits(v_new, shape, rows),
@@ -421,6 +452,7 @@ def lrqk_pages_append(shape, pages, k_new, v_new, stream=None):
 
 
 def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
+    _hold(pages, shape)
     rows = shape.B * shape.Hkv * (shape.l_cap if shape.l_cap > 0 else shape.l_max)
     _check(load_library().lrqk_pages_read(C.byref(shape), C.byref(pages), int(first),
                                           _fits(K_out, shape, rows, pinned=True),
@@ -429,6 +461,7 @@ def lrqk_pages_read(shape, pages, first, K_out, V_out, stream=None):
 
 
 def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
+    _hold(pages, shape)
     rows = shape.T * shape.Hq
     if workspace.device != out.device:
         raise ValueError(f"workspace on {workspace.device}, out on {out.device}")

@@ -108,3 +108,86 @@ def test_binding_refuses_what_is_no_device_tensor(lib):
         lib.lrqk_chunk_attend(s, p, rows, rows, rows, stream=0)              # host memory
     with pytest.raises(ValueError):
         lib.lrqk_pages_read(s, p, 0, torch.zeros(2, 4, 1000, 128, dtype=torch.bfloat16), None, stream=0)  # not pinned
+
+
+def held(lib, monkeypatch, **kw):
+    """Pages whose tensors fit good(lib, page_dtype=2), but for what is given; in host memory, taken for a device's."""
+    from paper_2510_23649_amd import binding
+    t = dict(K=torch.zeros(200, 4, 16, 128, dtype=torch.uint8), V=torch.zeros(200, 4, 16, 128, dtype=torch.uint8),
+             K_scale=torch.zeros(200, 4, 16, 4, dtype=torch.uint8), V_scale=torch.zeros(200, 4, 16, 4, dtype=torch.uint8),
+             table=torch.zeros(2, 63, dtype=torch.int32), start=torch.zeros(3, dtype=torch.int32),
+             kv_len=torch.zeros(2, dtype=torch.int32))
+    t.update(kw)
+    monkeypatch.setattr(binding, "_dev", lambda x, dtype=None: None if x is None else 0x10000)
+    monkeypatch.setattr(binding, "_raw_stream", lambda *a: 0)
+    return lib.make_pages(**t)
+
+
+def calls(lib, s, p):
+    """Every call on pages p, as it begins: what it would pass on to the library is not there."""
+    for f in (lambda: lib.lrqk_pages_append(s, p, None, None), lambda: lib.lrqk_pages_read(s, p, 0, None, None),
+              lambda: lib.lrqk_chunk_attend(s, p, None, torch.zeros(1), torch.zeros(1))):
+        yield f
+
+
+def test_pages_that_do_not_hold_the_shape(lib, monkeypatch):
+    """Pools, scales and tables of other types and sizes than the shape says: errors, and nothing launched."""
+    u8, i32 = torch.uint8, torch.int32
+    short = {"K": torch.zeros(199, 4, 16, 128, dtype=u8), "V": torch.zeros(200, 4, 16, 127, dtype=u8),
+             "K_scale": torch.zeros(200, 4, 16, 3, dtype=u8), "V_scale": torch.zeros(0, dtype=u8),
+             "table": torch.zeros(1, 125, dtype=i32), "start": torch.zeros(2, dtype=i32), "kv_len": torch.zeros(1, dtype=i32)}
+    s = good(lib, page_dtype=2)
+    for name, t in short.items():
+        for f in calls(lib, s, held(lib, monkeypatch, **{name: t})):
+            with pytest.raises(ValueError, match=name):
+                f()
+    p = held(lib, monkeypatch)
+    for kw in (dict(n_pages=201), dict(B=3), dict(max_pages=64), dict(max_pages=200, page=8), dict(Hkv=8, Hq=32), dict(page=32)):
+        for f in calls(lib, good(lib, **{"page_dtype": 2, **kw}), p):
+            with pytest.raises(ValueError):
+                f()
+    # the table's rows lie max_pages entries apart
+    wide = held(lib, monkeypatch, table=torch.zeros(2, 70, dtype=i32))
+    for f in calls(lib, s, wide):
+        with pytest.raises(ValueError, match="table"):
+            f()
+
+
+def test_pages_of_another_type_than_the_shape_says(lib, monkeypatch):
+    pool = lambda t: dict(K=torch.zeros(200, 4, 16, 128, dtype=t), V=torch.zeros(200, 4, 16, 128, dtype=t))  # noqa: E731
+    for t, kw in ((torch.float32, dict(page_dtype=0)), (torch.bfloat16, dict(kv_dtype=1, page_dtype=1)),
+                  (torch.bfloat16, dict(page_dtype=2)), (torch.float32, dict(kv_dtype=1, page_dtype=3)),
+                  (torch.uint8, dict(page_dtype=0)), (torch.uint8, dict(kv_dtype=1, page_dtype=1))):
+        for f in calls(lib, good(lib, **kw), held(lib, monkeypatch, **pool(t))):
+            with pytest.raises(TypeError):
+                f()
+
+
+def test_pages_that_hold_the_shape(lib, monkeypatch):
+    """What fits goes on to the library, which refuses the pointers that are not there; a bad shape is its to refuse."""
+    u8 = torch.uint8
+    fits = [(good(lib, page_dtype=2), {}), (good(lib, page_dtype=3), {}), (good(lib, n_pages=100, page_dtype=2), {}),
+            (good(lib, B=1, page_dtype=2), {}), (good(lib, B=1, max_pages=126, page_dtype=2), {}),
+            (good(lib, page_dtype=2), dict(K=torch.zeros(200, 4, 16, 128, dtype=torch.int8), V=torch.zeros(200, 4, 16, 128, dtype=torch.int8))),
+            (good(lib, page_dtype=2), dict(K=torch.zeros(200, 4, 16, 128).to(torch.float8_e4m3fn), V=torch.zeros(200, 4, 16, 128).to(torch.float8_e4m3fn))),
+            (good(lib, page_dtype=2), dict(table=torch.zeros(126, dtype=torch.int32))),
+            (good(lib, page_dtype=2), dict(K=torch.zeros(200 * 4 * 16 * 128, dtype=u8))),
+            (good(lib), dict(K=torch.zeros(200, 4, 16, 128, dtype=torch.bfloat16), V=torch.zeros(200, 4, 16, 128, dtype=torch.bfloat16), K_scale=None, V_scale=None)),
+            (good(lib, page_dtype=2), dict(K_scale=None, V_scale=None))]
+    for s, kw in fits:
+        p = held(lib, monkeypatch, **kw)
+        for _ in range(2):                   # found, and found again
+            for f in list(calls(lib, s, p))[:2]:
+                with pytest.raises(lib.LrqkError) as e:
+                    f()
+                assert e.value.status == -1
+    p = held(lib, monkeypatch)
+    for f in list(calls(lib, good(lib, page=24, n_pages=1 << 20, page_dtype=2), p))[:2]:
+        with pytest.raises(lib.LrqkError) as e:
+            f()
+        assert e.value.status == -2
+    # another shape after one that fits
+    lib_s, bad = good(lib, page_dtype=2), good(lib, page_dtype=2, n_pages=300)
+    for s, err in ((lib_s, lib.LrqkError), (bad, ValueError), (lib_s, lib.LrqkError)):
+        with pytest.raises(err):
+            lib.lrqk_pages_append(s, p, None, None)
