@@ -388,14 +388,20 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
 
 
 _PAGE_ROWS = {LRQK_PAGE_BF16: (torch.bfloat16,), LRQK_PAGE_F32: (torch.float32,)}
+# what of a shape says how much its pages hold: B, Hkv and d, page to max_pages, page_dtype
+_HELD = [slice(getattr(PagesShape, a).offset, getattr(PagesShape, b).offset + 4)
+         for a, b in (("B", "B"), ("Hkv", "d"), ("page", "max_pages"), ("page_dtype", "page_dtype"))]
 
 
 def _hold(pages: Pages, shape: PagesShape):
     """The tensors of make_pages have the types that `shape` says and at least its sizes: a kernel reaches
-    nothing beside them.  What a shape was found to fit is not looked at again until another one comes (0.2 us
-    of a call, 3 if it is looked at).  Pages made from raw pointers are the caller's."""
-    key = bytes(shape)
-    if getattr(pages, "tensors", None) is None or pages.fits == key:
+    nothing beside them.  What they were found to hold is not looked at again until another pool or table is
+    meant (0.4 us of a call, 8 if it is looked at).  Pages made from raw pointers are the caller's."""
+    if getattr(pages, "tensors", None) is None:
+        return
+    raw = bytes(shape)
+    key = raw[_HELD[0]] + raw[_HELD[1]] + raw[_HELD[2]] + raw[_HELD[3]]
+    if pages.fits == key:
         return
     if lrqk_validate_pages(shape) != 0:
         return                               # the call says so

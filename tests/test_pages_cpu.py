@@ -191,3 +191,18 @@ def test_pages_that_hold_the_shape(lib, monkeypatch):
     for s, err in ((lib_s, lib.LrqkError), (bad, ValueError), (lib_s, lib.LrqkError)):
         with pytest.raises(err):
             lib.lrqk_pages_append(s, p, None, None)
+
+
+def test_what_was_found_to_fit_is_found_again(lib, monkeypatch):
+    """Another number of tokens or another length means the same pages; each of what says how much they hold does not."""
+    from paper_2510_23649_amd import binding
+    p, s = held(lib, monkeypatch), good(lib, page_dtype=2)
+    binding._hold(p, s)
+    looked = []
+    monkeypatch.setattr(binding, "lrqk_validate_pages", lambda x: looked.append(1) or -1)
+    for kw in ({}, dict(T=100, n_max=90), dict(l_max=700, l_cap=800), dict(Hq=8, scale=2.0)):
+        binding._hold(p, good(lib, page_dtype=2, **kw))
+    assert not looked
+    for kw in (dict(B=1), dict(Hkv=2), dict(d=64), dict(page=8), dict(n_pages=100), dict(max_pages=64), dict(page_dtype=3)):
+        binding._hold(p, good(lib, **{"page_dtype": 2, **kw}))
+        assert looked.pop()
