@@ -455,8 +455,10 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  * 8-bit pages: every 32 elements of a row share a scale 2^e, the smallest power of two with
  * e >= -110 for which none of them exceeds the largest code (448 for e4m3, 127 for i8), kept as the
  * byte e + 127.  Codes are x 2^-e rounded to the nearest, ties to even; since the scale is a power of
- * two that is the only rounding, and a code times its scale is exact in bf16 and fp32.  32
- * elements with an infinity or a NaN among them get the scale byte 255 and read as NaN.
+ * two that is the only rounding, and a code times its scale is exact in bf16 and fp32.  A finite
+ * element is read back finite: where the nearest code would mean 2^128 (bf16's largest number does) the
+ * next one below is taken.  32 elements with an infinity or a NaN among them get the scale byte 255 and
+ * read as NaN.
  */
 enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 = 3 };
 

@@ -114,23 +114,28 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   return (uint32_t)(max(e, kMinExp) + 127);
 }
 
-// Eight elements as codes of a block with that scale byte.
+// Eight elements as codes of a block with that scale byte.  With the largest scale (that of a block whose largest magnitude is
+// above 448 2^119 or 127 2^121) a number may lie nearest to 256 2^120 or 64 2^122, which is 2^128: it takes the code below, so
+// that what is finite is read back finite.
 template <int PAGE>
 __device__ __forceinline__ uint2 encode8(const float (&x)[8], uint32_t byte) {
   if (byte == 255u) return make_uint2(0u, 0u);
   const float inv = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte), a normal number
+  constexpr bool kE4m3 = PAGE == LRQK_PAGE_E4M3;
+  const float most = byte >= (kE4m3 ? 247u : 249u) ? (kE4m3 ? 240.0f : 63.0f) : (kE4m3 ? 448.0f : 127.0f);
+  auto scaled = [&](int i) { return __builtin_amdgcn_fmed3f(x[i] * inv, -most, most); };
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if constexpr (PAGE == LRQK_PAGE_E4M3) {
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inv, x[4 * i + 1] * inv, 0, false);
-      v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inv, x[4 * i + 3] * inv, v, true);
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i), scaled(4 * i + 1), 0, false);
+      v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i + 2), scaled(4 * i + 3), v, true);
       w[i] = (uint32_t)v;
     } else {
       uint32_t v = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        v |= ((uint32_t)(int)__builtin_rintf(x[4 * i + j] * inv) & 0xffu) << (8 * j);
+        v |= ((uint32_t)(int)__builtin_rintf(scaled(4 * i + j)) & 0xffu) << (8 * j);
       w[i] = v;
     }
   }

@@ -1,0 +1,72 @@
+"""GPU tests of the paged cache at the ends of the number range.  Cases, plain forms and bounds are those of
+tests/test_gpu_pages.py unless a test says otherwise."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_23649_amd as L
+import pages_plain as P
+from test_gpu_pages import DEV, D, MARK, Case
+
+pytestmark = pytest.mark.gpu
+E8 = [("bf16", "e4m3"), ("bf16", "i8"), ("f32", "e4m3"), ("f32", "i8")]
+BIGGEST = {"bf16": float(torch.finfo(torch.bfloat16).max), "f32": float(torch.finfo(torch.float32).max)}
+
+
+# ---- rows written in 8 bits --------------------------------------------------------------------------
+def quantise(x, pages):
+    """P.quantise, but that no finite element becomes 2^128, which neither bf16 nor fp32 holds: the next lower code."""
+    code, byte = P.quantise(x, pages)
+    top = np.repeat(byte == (247 if pages == "e4m3" else 249), 32, axis=-1)
+    if pages == "e4m3":                      # 256 * 2^120 -> 240 * 2^120
+        code = np.where(top & ((code & 0x7F) == 0x78), code - 1, code)
+    else:                                    # 64 * 2^122 -> 63 * 2^122
+        code = np.where(top & (code == 64), 63, np.where(top & (code == 192), 193, code))
+    return code.astype(np.uint8), byte
+
+
+def special_blocks(kv, pages, g):
+    """Blocks of 32 elements at which a scale or a rounding can go wrong, as rows of 128 (four blocks a row)."""
+    top, dt, big = P.TOP[pages], P.TYPE[kv], BIGGEST[kv]
+    up = lambda x, to: float(torch.nextafter(torch.tensor(x, dtype=dt), torch.tensor(to, dtype=dt)))  # noqa: E731
+    rnd = lambda: torch.randn(32, generator=g, dtype=torch.float64)  # noqa: E731
+    one = lambda v, i=9: rnd().index_fill_(0, torch.tensor(i), v)  # noqa: E731
+    steps = torch.arange(32, dtype=torch.float64)
+    blocks = [torch.zeros(32), -torch.zeros(32), torch.full((32,), 3.0e38), torch.full((32,), 1.0e-30), torch.full((32,), 1.0e-40),
+              torch.linspace(-top, top, 32), one(up(top, big), 0), one(-up(top, big)), one(up(top, 0.0)), one(top * 2.0 ** -110),
+              torch.full((32,), -top * 2.0 ** -112), (steps * 0.5 + 0.25).index_fill_(0, torch.tensor(31), top),
+              (steps + 0.5).index_fill_(0, torch.tensor(31), -top), one(float("nan"), 3), one(float("inf")), one(-float("inf")),
+              # the largest finite numbers, and those around the last one that rounds down to a code whose value is finite
+              torch.full((32,), big), -torch.full((32,), big), one(big), one(-big, 31), one(up(big, 0.0)),
+              torch.linspace(-1.0, 1.0, 32, dtype=torch.float64) * big, torch.linspace(0.9, 1.0, 32, dtype=torch.float64) * big,
+              one(247.0 * 2.0 ** 120), one(248.0 * 2.0 ** 120), one(-249.0 * 2.0 ** 120), one(1.75 * 2.0 ** 127),
+              one(up(1.75 * 2.0 ** 127, big)), one(127.0 * 2.0 ** 121), one(up(127.0 * 2.0 ** 121, big)), one(-2.0 ** 127)]
+    blocks += [rnd() for _ in range(-len(blocks) % 4)]
+    return torch.stack([b.to(torch.float64) for b in blocks]).view(-1, 128).to(dt)
+
+
+@pytest.mark.parametrize("kv,pages", E8)
+@pytest.mark.parametrize("page,Hkv", [(16, 1), (4, 2), (64, 3)])
+def test_special_blocks_are_written_and_read(page, Hkv, kv, pages):
+    """Every special block in K and in V of tokens that belong to a sequence and have a page; finite elements stay finite."""
+    x = special_blocks(kv, pages, torch.Generator().manual_seed(7))
+    n = -(-x.shape[0] // Hkv)
+    c = Case([(n, n + 5), (1, 3)], Hkv, 2, page, kv, pages, seed=60, front=2, back=3)
+    x = torch.cat([x, x[:n * Hkv - x.shape[0]]])
+    c.k_new[2:2 + n] = x.view(n, Hkv, D)
+    c.v_new[2:2 + n] = x.flip(0).view(n, Hkv, D)
+    assert all(c.where(0, 5 + i) is not None for i in range(n)) and int(c.start[0]) == 2 and int(c.start[1]) == 2 + n
+    c.to_device()
+    L.lrqk_pages_append(c.shape, c.pg, c.k_new.to(DEV), c.v_new.to(DEV))
+    out = {a: torch.full((2, Hkv, n + 5, D), MARK, dtype=P.TYPE[kv], device=DEV) for a in "KV"}
+    L.lrqk_pages_read(c.shape, c.pg, 0, out["K"], out["V"])
+    for name, new in (("K", c.k_new), ("V", c.v_new)):
+        code, byte = quantise(new[2:2 + n].double().numpy(), pages)
+        at = [c.where(0, 5 + i) for i in range(n)]
+        pg, off = [a[0] for a in at], [a[1] for a in at]
+        assert np.array_equal(c.ds[name].cpu().numpy()[pg, :, off], byte), f"{name}: scales"
+        assert np.array_equal(c.d[name].cpu().numpy()[pg, :, off], code), f"{name}: codes"
+        got = out[name][0, :, 5:].transpose(0, 1).double().cpu().numpy()
+        assert np.array_equal(got, P.values(code, byte, pages), equal_nan=True), f"{name}: values"
+        fine = np.isfinite(new[2:2 + n].double().numpy().reshape(n, Hkv, 4, 32)).all(-1)
+        assert np.isfinite(got.reshape(n, Hkv, 4, 32)).all(-1)[fine].all(), f"{name}: a finite element is read as an infinity"
