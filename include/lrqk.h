@@ -458,7 +458,8 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  * two that is the only rounding, and a code times its scale is exact in bf16 and fp32.  A finite
  * element is read back finite: where the nearest code would mean 2^128 (bf16's largest number does) the
  * next one below is taken.  32 elements with an infinity or a NaN among them get the scale byte 255 and
- * read as NaN.
+ * read as NaN.  Pools that are not written by lrqk_pages_append may hold other codes and scales, -128 and the
+ * NaN of e4m3 too: a product that kv_dtype does not hold is an infinity.
  */
 enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 = 3 };
 

@@ -662,9 +662,16 @@ __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows,
       const int64_t at = row_of(a.m, p.b, kvh, pos);
       if (at < 0) continue;
       float v;
-      if constexpr (is8(PAGE)) {
-        const bool nan = PAGE == LRQK_PAGE_E4M3 && (static_cast<const uint8_t*>(a.V)[at * kD + d] & 0x7f) == 0x7f;
-        v = nan || a.V_scale[at * kScales + d / kScaleBlock] == 255 ? NAN : 0.0f;
+      if constexpr (is8(PAGE)) {  // as Block::widen makes it: a pool from elsewhere may hold what exceeds the type
+        const uint2 code = make_uint2(static_cast<const uint8_t*>(a.V)[at * kD + d], 0u);
+        const float scale = scale_of(a.V_scale[at * kScales + d / kScaleBlock]);
+        if constexpr (BF16) {
+          v = __uint_as_float(decode8_bf16<PAGE>(code, scale).x << 16);
+        } else {
+          float f[8];
+          decode8<PAGE>(code, scale, f);
+          v = f[0];
+        }
       } else if constexpr (PAGE == LRQK_PAGE_BF16) {
         v = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.V)[at * kD + d] << 16);
       } else {

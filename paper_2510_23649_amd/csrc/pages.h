@@ -82,8 +82,8 @@ __device__ __forceinline__ void decode8(uint2 c, float s, float (&x)[8]) {
   }
 }
 
-// The same as four packed bf16 pairs: exact too (a code has at most seven bits, and scales as they are written leave bf16's
-// range of normal numbers by no means).
+// The same as four packed bf16 pairs: exact too (a code has at most seven bits, and with scales as they are written the product
+// is a normal number of bf16 or 0; with larger ones, in a pool from elsewhere, it may be an infinity).
 template <int PAGE>
 __device__ __forceinline__ uint4 decode8_bf16(uint2 c, float s) {
   if constexpr (PAGE == LRQK_PAGE_E4M3) {

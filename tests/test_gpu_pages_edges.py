@@ -10,6 +10,8 @@ from test_gpu_pages import DEV, D, MARK, Case
 
 pytestmark = pytest.mark.gpu
 E8 = [("bf16", "e4m3"), ("bf16", "i8"), ("f32", "e4m3"), ("f32", "i8")]
+# (new tokens, length) of the first sequence, with three heads a group: one row a wavefront, 33 to 64 rows, more
+WAYS = {"one": (1, 40), "thin": (9, 75), "pair": (14, 75), "tile": (70, 150)}
 BIGGEST = {"bf16": float(torch.finfo(torch.bfloat16).max), "f32": float(torch.finfo(torch.float32).max)}
 
 
@@ -70,3 +72,26 @@ def test_special_blocks_are_written_and_read(page, Hkv, kv, pages):
         assert np.array_equal(got, P.values(code, byte, pages), equal_nan=True), f"{name}: values"
         fine = np.isfinite(new[2:2 + n].double().numpy().reshape(n, Hkv, 4, 32)).all(-1)
         assert np.isfinite(got.reshape(n, Hkv, 4, 32)).all(-1)[fine].all(), f"{name}: a finite element is read as an infinity"
+
+
+# ---- infinities in V ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("kv,pages", E8)
+@pytest.mark.parametrize("way", WAYS)
+def test_codes_too_large_for_the_type(way, kv, pages):
+    """A pool from elsewhere may hold codes whose value exceeds bf16 and fp32: infinities for the tokens that see them."""
+    n, ln = WAYS[way]
+    c = Case([(n, ln), (2, 40)], 1, 3, 16, kv, pages, seed=61)
+    for p, d, minus in ((ln - 1, 5, False), (ln - max(1, n // 2), 40, True), (ln - n, 70, False), (2, 100, True)):
+        pg, o = c.where(0, p)
+        c.pool["V"][pg, 0, o, d // 32 * 32:d // 32 * 32 + 32] = 0
+        c.pool["V"][pg, 0, o, d] = (0x7E if pages == "e4m3" else 0x7F) if not minus else (0xFE if pages == "e4m3" else 0x81)
+        c.sc["V"][pg, 0, o, d // 32] = 254
+    rows = c.rows
+
+    def as_held(name, b):
+        x, there = rows(name, b)
+        return np.where(np.abs(x) > BIGGEST["f32"], np.copysign(np.inf, x), x), there
+
+    c.rows = as_held
+    c.to_device()
+    c.check_attend(c.attend())
