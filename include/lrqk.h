@@ -525,7 +525,8 @@ int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pages, int3
  *   out[start[b]+i,h,:] = sum_{p <= p0} w_p V_p,   w = softmax_p(scale * q[start[b]+i,h,:] . K_p)
  * over the positions that exist (their pages too), K and V of KV head h / G.  A token that sees no
  * position, or only scores of -infinity, gets zeros.  What a token does not see does not reach its
- * output, whatever its rows hold.  Products of bf16 operands are exact, sums fp32; with bf16 q the
+ * output, whatever its rows hold.  An infinite element of V under a weight of 0 (a score of -infinity, or one
+ * that far below the others) makes NaN or that infinity.  Products of bf16 operands are exact, sums fp32; with bf16 q the
  * weights are rounded to bf16 before they meet V and before they are summed.
  *   q    device kv_dtype [T,Hq,d]
  *   out  device kv_dtype [T,Hq,d]  written

@@ -650,12 +650,17 @@ __device__ __forceinline__ void put(const Args& a, const Problem& p, int kvh, in
 }
 
 // Elements of V that are not finite at positions [from, to) that some rows of the workgroup see and others do not were left
-// out: each row gets those that it sees, a thread per element.  Rare, and slow.
+// out: each row gets those that it sees, a thread per element.  Rare, and slow.  sums: of row r's weights, those of state v at
+// v * rows_held + r; a row of the output without any (its scores are -infinity) stays 0.
 template <bool BF16, int PAGE>
-__device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows, int piece, int from, int to) {
+__device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows, int piece, int from, int to,
+                             const float* sums, int states, int rows_held) {
   __syncthreads();  // what this workgroup has written is read below
   const int d = threadIdx.x % kD;
   for (int r = threadIdx.x / kD; r < rows; r += kThreads / kD) {
+    bool any = a.partials != nullptr;  // (the join's to say)
+    for (int v = 0; v < states; ++v) any |= sums[v * rows_held + r] != 0.0f;
+    if (!any) continue;
     const int row = p.r0 + r, end = min(to, sees(a, p, row));
     float x = 0.0f;
     for (int pos = from; pos < end; ++pos) {
@@ -899,6 +904,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
   constexpr int M = 128, BN = Loop::BN, kTile = BN * kRowB<BF16>;
   __shared__ __align__(16) char kt0[kTile], vt0[kTile], kt1[kTile], vt1[kTile];
   __shared__ __align__(8) uint16_t there[4][4];
+  __shared__ float sums[M];
   // KV head fastest: the dies take workgroups in turn, so a head's rows stay in one die's L2
   const int kvh = blockIdx.x % a.m.Hkv;
   Problem p;
@@ -921,6 +927,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
     cleared = loop.cleared;
   }
   r.sum = sum_halves(r.sum);
+  if (lane < 32) sums[w * 32 + lane] = r.sum;
   if (mine < p.rows) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -929,7 +936,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) 
         put<BF16>(a, p, kvh, mine, p.piece, 32 * t + 8 * e + 4 * (lane >> 5),
                   f32x4{r.o[t][4 * e], r.o[t][4 * e + 1], r.o[t][4 * e + 2], r.o[t][4 * e + 3]}, r.mx, r.sum);
   }
-  if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
+  if (__syncthreads_or(cleared))
+    add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, sums, 1, M);
 }
 
 // The states of several wavefronts at the same rows joined and put: `n` of them, that of state v and row i at
@@ -1028,7 +1036,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
     leave_state(r, w * M, lane, reinterpret_cast<float*>(lds), wm, ws);
     __syncthreads();
     join_states<BF16>(a, p, kvh, rows, kWaves, M, reinterpret_cast<const float*>(lds), wm, ws);
-    if (__syncthreads_or(cleared)) add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
+    if (__syncthreads_or(cleared))
+      add_left_out<BF16, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, kWaves, M);
   }
 }
 
@@ -1069,7 +1078,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) 
     leave_state(r, half * M + 32 * set, lane, reinterpret_cast<float*>(lds), wm, ws);
     __syncthreads();
     join_states<true>(a, p, kvh, rows, 2, M, reinterpret_cast<const float*>(lds), wm, ws);
-    if (__syncthreads_or(cleared)) add_left_out<true, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end);
+    if (__syncthreads_or(cleared))
+      add_left_out<true, PAGE>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, 2, M);
   }
 }
 

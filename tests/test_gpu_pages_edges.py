@@ -95,3 +95,19 @@ def test_codes_too_large_for_the_type(way, kv, pages):
     c.rows = as_held
     c.to_device()
     c.check_attend(c.attend())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("v", [0.0, float("inf"), float("nan")], ids=["finite", "inf", "nan"])
+def test_scores_of_minus_infinity_alone(v, way, kv):
+    """Tokens that see only scores of -infinity get zeros, whatever the rows of V hold."""
+    n, ln = WAYS[way]
+    c = Case([(n, ln), (1, 1)], 1, 3, 16, kv, kv, seed=63)
+    c.q[..., 0], c.q[..., 1:] = 1.0, 0.0
+    c.pool["K"][..., 0] = -float("inf")
+    for p, d in ((ln - 1, 3), (ln - n, 60), (2, 127)):
+        pg, o = c.where(0, p)
+        c.pool["V"][pg, 0, o, d] = v
+    c.to_device()
+    assert (c.attend() == 0).all()
