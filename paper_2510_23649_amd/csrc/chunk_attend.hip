@@ -42,6 +42,7 @@ constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.0f;
 constexpr float kHeavy = 4096.0f;
+constexpr float kFar = 1073741824.0f;  // see Rows::weigh
 constexpr int kPartial = kPartialStride;  // floats of a partial state: max, sum, 2 unused, acc[128]
 
 struct Args {
@@ -408,6 +409,7 @@ struct Rows {
   uint4 q[BF16 ? 8 : 16];  // bf16: elements 16 s + 8 h .. + 7; fp32: 8 s + 4 h .. + 3
   f32x16 o[4];             // elements 32 t .. of O^T
   float mx, sum;           // of what has been seen, in units of log2
+  float near;              // mx; -infinity where that is no number below kFar
   int see;                 // positions that the lane's row sees
 
   __device__ __forceinline__ void start(const void* base, int64_t row, bool negate, int lane) {
@@ -424,6 +426,7 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
     mx = -INFINITY;
+    near = -INFINITY;
     sum = 0.0f;
   }
 
@@ -462,12 +465,29 @@ struct Rows {
     for (int e = 0; e < 16; ++e) s[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? s[e] : -INFINITY;
   }
 
-  // weights of 32 positions at the running maximum
-  __device__ __forceinline__ f32x16 weigh(const f32x16& s, float c) const {
-    const float base = mx == -INFINITY ? 0.0f : mx;
+  // Weights of 32 positions at the running maximum.  That is rounded, and s c inside the instruction is not: what lies between them
+  // is a factor that all weights of the row share, of 2^+-32 at most as long as the maximum is below kFar = 2^30.  Where it is not,
+  // or where there is none yet, `near` makes them infinite or NaN, for who takes them to look at their sum.
+  __device__ __forceinline__ f32x16 weigh(const f32x16& s, float c, float base) const {
     f32x16 w;
 #pragma unroll
     for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base));
+    return w;
+  }
+  // The row's maximum is beyond that, or there is none.
+  __device__ __forceinline__ bool far() const { return fabsf(mx) >= kFar; }
+  // The same for every row: those beyond kFar with products that are rounded like the maximum, so that the largest score has the
+  // weight 1.
+  __device__ __forceinline__ f32x16 weigh_any(const f32x16& s, float c) const {
+#pragma clang fp contract(off)
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    const bool rounded = far();
+    f32x16 w;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = s[e] * c;
+      w[e] = __builtin_amdgcn_exp2f(rounded ? y - base : __builtin_fmaf(s[e], c, -base));
+    }
     return w;
   }
   // the largest score of the row, in units of log2
@@ -487,6 +507,7 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[t][e] *= f;
     mx = to;
+    near = fabsf(to) < kFar ? to : -INFINITY;
   }
 
   struct Weights {  // of 32 positions as the second product's operand
@@ -527,7 +548,11 @@ struct Rows {
     };
     const float top = largest(s, c);
     if (__any(top > mx + kLag)) raise(top);  // (-inf > -inf is false: nothing seen so far, nothing to do)
-    const auto x = form(weigh(s, c));
+    auto x = form(weigh(s, c, mx == -INFINITY ? 0.0f : mx));
+    if (__builtin_expect(__any(far()), 0)) {
+      asm volatile("");  // a branch, which next to no call takes
+      x = form(weigh_any(s, c));
+    }
     sum += add_up(x);
     return x;
   }
@@ -587,7 +612,7 @@ struct Rows {
       next = scores_step(kt, k, next, lane);
       if (BEFORE) output_step(vt, x, k >> 2, k & 3, lane);
     }
-    x = pack(weigh(s, c));
+    x = pack(weigh(s, c, near));
     float add = add_up(x);
     // made here, between the products, and not only once the maximum is known to stand
     asm volatile("" : "+v"(x.half[0].x), "+v"(x.half[0].y), "+v"(x.half[0].z), "+v"(x.half[0].w), "+v"(x.half[1].x),
@@ -608,10 +633,10 @@ struct Rows {
       }
     }
     // The sum says whether the maximum has to be raised, without the scores being looked through for theirs (eight of some 55
-    // vector instructions).  Where there is no maximum yet the weights may be nothing.
-    if (__any(add > kHeavy || mx == -INFINITY)) {
+    // vector instructions).  Where there is no maximum yet, or a far one, it is no number that is less.
+    if (__any(!(add <= kHeavy))) {
       raise(largest(s, c));
-      x = pack(weigh(s, c));
+      x = pack(weigh_any(s, c));
       add = add_up(x);
     }
     sum += add;

@@ -111,3 +111,61 @@ def test_scores_of_minus_infinity_alone(v, way, kv):
         c.pool["V"][pg, 0, o, d] = v
     c.to_device()
     assert (c.attend() == 0).all()
+
+
+# ---- scores --------------------------------------------------------------------------------------------
+LONG = dict(WAYS, one_in_pieces=(1, 3000), pair_in_pieces=(14, 3000), tile_in_pieces=(50, 3000))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("way", LONG)
+def test_huge_scores_all_alike(way, kv):
+    """Scores are q . K = v exactly and all alike, so that every weight is exactly 1 and the output the mean of what is
+    seen: off by its own rounding, those of the two sums over L positions and two for the quotient."""
+    n, ln = LONG[way]
+    c = Case([(n, ln)], 1, 3, 16, kv, kv, seed=65)
+    c.q[..., 0], c.q[..., 1:] = 1.0, 0.0
+    c.pool["K"][:] = 0.0
+    V, _ = c.rows("V", 0)
+    many = np.arange(ln - n, ln)[:, None] + 1.0
+    y, mass = (np.cumsum(x, 0)[ln - n:, None] / many[:, None] for x in (V[0], np.abs(V[0])))
+    tol = (2.0 ** -8 if kv == "bf16" else 2.0 ** -24) * np.abs(y) + mass * (2 * ln + 2) * 2.0 ** -24
+    c.to_device()
+    for v in (-3.0e38, 3.0e38, -1.0e30, 1.0e12, -5.0e9, 1.0e6):
+        c.d["K"][..., 0] = v
+        got = c.attend().double().cpu().numpy()
+        assert (np.abs(got - y) <= tol).all(), (v, np.abs(got - y).max())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("way", LONG)
+@pytest.mark.parametrize("order", ["grows", "falls", "mixed"])
+def test_huge_scores_far_apart(order, way, kv):
+    """Scores that are multiples of a large power of two, exactly: all weight on the largest, whose row of V is the output.
+    (Scores differ by 2^22 sqrt(1 / 128) at least: what the others count for is 0.)  Its weight w need not be 1, since the
+    maximum that it is taken at is rounded: y = fl(fl(w V) fl(1 / w)) has three roundings in fp32, (1 + 2^-24)^3 - 1 < 3.001 2^-24;
+    in bf16 fl(w V) of two bf16 numbers is exact and the output's rounding takes the other two back: nothing is off."""
+    n, ln = LONG[way]
+    first = ln - n
+    c = Case([(n, ln)], 1, 3, 16, kv, kv, seed=66)
+    c.q[..., 0], c.q[..., 1:] = 1.0, 0.0
+    c.pool["K"][:] = 0.0
+    V, _ = c.rows("V", 0)
+    m = np.zeros(ln)                         # 1 .. 240 (8 bits: exact in bf16) at some positions, 0 at the others
+    some = np.linspace(0, ln - 1, min(ln, 240)).astype(np.int64)
+    m[some] = np.arange(1, len(some) + 1)
+    if order == "falls":
+        m = m[::-1].copy()
+    elif order == "mixed":
+        m[some] = np.random.default_rng(67).permutation(m[some])
+    best = np.array([int(np.argmax(m[:i + 1])) for i in range(first, ln)])
+    assert all((np.delete(m[:i + 1], j) < m[j]).all() for i, j in zip(range(first, ln), best)), "one largest score a token"
+    c.to_device()
+    at = [c.where(0, p) for p in range(ln)]
+    for unit, off in ((2.0 ** 113, 0.0), (2.0 ** 113, 250.0), (2.0 ** 40, 0.0), (2.0 ** 30, 250.0), (2.0 ** 26, 0.0), (2.0 ** 22, 250.0)):
+        k = torch.from_numpy(unit * (m - off)).to(P.TYPE[kv])
+        assert np.array_equal(k.double().numpy(), unit * (m - off))
+        c.d["K"][[a[0] for a in at], 0, [a[1] for a in at], 0] = k.to(DEV)
+        got = c.attend().double().cpu().numpy()
+        y = np.repeat(V[0, best][:, None], 3, axis=1)
+        assert (np.abs(got - y) <= (0.0 if kv == "bf16" else 3.001 * 2.0 ** -24) * np.abs(y)).all(), (unit, off)
