@@ -1,12 +1,13 @@
-"""GPU tests of the paged cache at the ends of the number range.  Cases, plain forms and bounds are those of
-tests/test_gpu_pages.py unless a test says otherwise."""
+"""GPU tests of the paged cache at the ends of the number range: rows near the largest finite numbers, scores that are
+huge, of the lowest value or of -infinity, infinities that only some tokens see, contexts of 128K.  Cases, plain
+forms and bounds are those of tests/test_gpu_pages.py unless a test says otherwise."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2510_23649_amd as L
 import pages_plain as P
-from test_gpu_pages import DEV, D, MARK, Case
+from test_gpu_pages import DEV, D, MARK, Case, exact_on_device
 
 pytestmark = pytest.mark.gpu
 E8 = [("bf16", "e4m3"), ("bf16", "i8"), ("f32", "e4m3"), ("f32", "i8")]
@@ -99,6 +100,21 @@ def test_codes_too_large_for_the_type(way, kv, pages):
 
 @pytest.mark.parametrize("kv", ["bf16", "f32"])
 @pytest.mark.parametrize("way", WAYS)
+def test_infinities_reach_the_tokens_that_see_them(way, kv):
+    """Infinities and NaN in V rows of later tokens and of earlier ones, in K rows of later ones, for every shape of workgroup."""
+    n, ln = WAYS[way]
+    c = Case([(n, ln), (2, 40)], 2, 3, 16, kv, kv, seed=62)
+    for j, p in enumerate((ln - 1, ln - max(1, n // 2), ln - n, 1)):
+        pg, o = c.where(0, p)
+        c.pool["V"][pg, j % 2, o, 5 + j] = [float("inf"), float("-inf"), float("nan"), float("inf")][j]
+        if j == 0 and n > 1:
+            c.pool["K"][pg, 1, o, 3] = float("nan")
+    c.to_device()
+    c.check_attend(c.attend())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("way", WAYS)
 @pytest.mark.parametrize("v", [0.0, float("inf"), float("nan")], ids=["finite", "inf", "nan"])
 def test_scores_of_minus_infinity_alone(v, way, kv):
     """Tokens that see only scores of -infinity get zeros, whatever the rows of V hold."""
@@ -114,6 +130,21 @@ def test_scores_of_minus_infinity_alone(v, way, kv):
 
 
 # ---- scores --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("way", WAYS)
+def test_lowest_scores_beside_ordinary_ones(way, kv):
+    n, ln = WAYS[way]
+    c = Case([(n, ln), (1, 35)], 1, 3, 16, kv, kv, seed=64)
+    c.q[..., 0] = 1.0
+    for b, p, v in ((0, 7, -3.0e38), (0, ln - n, -float("inf")), (0, ln - n // 2 - 1, -3.0e38), (0, 33, -float("inf")), (1, 0, -3.0e38),
+                    (1, 34, -float("inf"))):
+        pg, o = c.where(b, p)
+        c.pool["K"][pg, :, o, 1:] = 0.0
+        c.pool["K"][pg, :, o, 0] = v
+    c.to_device()
+    c.check_attend(c.attend())
+
+
 LONG = dict(WAYS, one_in_pieces=(1, 3000), pair_in_pieces=(14, 3000), tile_in_pieces=(50, 3000))
 
 
@@ -169,3 +200,23 @@ def test_huge_scores_far_apart(order, way, kv):
         got = c.attend().double().cpu().numpy()
         y = np.repeat(V[0, best][:, None], 3, axis=1)
         assert (np.abs(got - y) <= (0.0 if kv == "bf16" else 3.001 * 2.0 ** -24) * np.abs(y)).all(), (unit, off)
+
+
+# ---- lengths -------------------------------------------------------------------------------------------
+ONES, PAIR, TILE = [(1, 131072), (1, 0), (1, 1)], [(13, 131072), (2, 131001)], [(40, 131071)]
+
+
+@pytest.mark.parametrize("seqs,kv,pages", [(ONES, "bf16", "e4m3"), (ONES, "f32", "f32"), (PAIR, "bf16", "i8"), (PAIR, "f32", "e4m3"),
+                                           (TILE, "bf16", "bf16"), (TILE, "bf16", "e4m3")])
+def test_128k(seqs, kv, pages):
+    c = Case(seqs, 1, 4, 256, kv, pages, seed=68).to_device()
+    out = c.attend().double()
+    for b in range(c.B):
+        lo, hi = int(c.start[b]), int(c.start[b + 1])
+        if c.len[b] == 0:
+            assert (out[lo:hi] == 0).all()
+            continue
+        y, mass, slack, Ln = exact_on_device(c, b)
+        half = 2.0 ** -8 if kv == "bf16" else 2.0 ** -24
+        tol = half * y.abs() + mass * (slack + 2 * Ln * 2.0 ** -24 + (2.0 ** -8 if kv == "bf16" else 0.0))
+        assert float(((out[lo:hi] - y).abs() - tol).max()) <= 0, f"sequence {b}"
