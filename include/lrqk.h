@@ -469,7 +469,8 @@ enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 =
  *              differ by roundings
  *   l_max      positions of any one sequence, at most, 1 <= l_max < 2^24
  *   l_cap      rows allocated per head in the dense arrays of lrqk_pages_read; 0 means l_max
- *   page       positions per page: a power of two, 1 <= page <= 1024
+ *   page       positions per page: a power of two, 1 <= page <= 1024; from 16 on for prompts, whose
+ *              attention takes twice as long over smaller ones
  *   n_pages    pages of the pool: at most 64 GiB of K rows and as much of V rows
  *   max_pages  entries of a sequence's row of the table, max_pages * page >= l_max
  *   kv_dtype   LRQK_KV_*: type of q, out, k_new, v_new and the dense arrays

@@ -917,12 +917,12 @@ struct PlainLoop {
 
 // 128 rows of the problem, 32 a wavefront.  Bound by the matrix cores and the vector instructions between their products: a
 // step of 32 positions has 16 products (32 cycles each) and some 65 vector instructions, and two wavefronts a SIMD are what
-// the registers allow.  2048 tokens at 32K, bf16, 32 + 8 heads: 1030 us, 1.03 PFLOP/s, matrix cores busy 44% of the cycles, no
-// LDS bank conflict; 8-bit rows are decoded once a workgroup, between the rounds (1024 tokens at 128K of e4m3: 2450 us,
-// 0.89 PFLOP/s).  64 rows a wavefront, one a SIMD, halve the decoding and the reads of LDS and took longer (1160 and 3007 us
+// the registers allow.  2048 tokens at 32K, bf16, 32 + 8 heads: 1040 to 1075 us from card to card, 1.0 PFLOP/s, matrix cores busy 45% of the cycles, no
+// LDS bank conflict; 8-bit rows are decoded once a workgroup, between the rounds (1024 tokens at 128K of e4m3: 2440 us,
+// 0.90 PFLOP/s).  64 rows a wavefront, one a SIMD, halve the decoding and the reads of LDS and took longer (1160 and 3007 us
 // where this took 1030 and 2560): what a wavefront waits for is then not covered by another one's products.  Decoding between a
-// step's products does not fit the registers (90 spilled).  fp32: 1001 tokens at 5003 and 744 at 1315, 660 us with the join, 113 TFLOP/s; 2048 tokens at 16K
-// 133 TFLOP/s of the 153 that a matrix product reaches.
+// step's products does not fit the registers (90 spilled).  fp32: 1001 tokens at 5003 and 744 at 1315, 665 us with the join, 112 TFLOP/s; 2048 tokens at 16K
+// 131 TFLOP/s of the 153 that a matrix product reaches.
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_tile_kernel(const Args a) {
   using Loop = std::conditional_t<BF16, TileLoop<PAGE>, PlainLoop<false, PAGE, 32>>;
@@ -1068,7 +1068,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
 
 // 33 to 64 rows: rows of the pool are read and decoded once for all of them, which a thin workgroup per 32 rows would do
 // twice.  Bound by the decoding and the barriers between blocks more than by memory.  1 to 5 tokens of 8 sequences of 7K to 64K,
-// 7 heads a group, i8, 192 MB: 63 us with the join, 3.0 TB/s (75 with pieces from the longest sequence alone: no more than 372 of the 512
+// 7 heads a group, i8, 192 MB: 64 us with the join, 3.0 TB/s (75 with pieces from the longest sequence alone: no more than 372 of the 512
 // workgroups had any; as thin workgroups with two sets of rows a wavefront 101).
 template <int PAGE>
 __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(const Args a) {
@@ -1193,7 +1193,9 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
 // How a call is cut up.  At most 32 rows a sequence and KV head go the thin way, and all calls with pages of less than 16
-// positions; up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit); more in tiles.
+// positions, whose rows have a place each (2048 tokens at 32K, bf16: 2360 us, and 1050 with pages of 16 and more; 12 tokens 38 and
+// 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
+// more in tiles.
 struct Cut {
   int rows;  // 32: thin, 64: pair, 128: tile
   int units, pieces, prefer, want, least;  // units: of a KV head, at most; the others: piece_of
@@ -1219,8 +1221,8 @@ Cut cut(const lrqk_pages_shape& s) {
   c.want = 0;
   if (most <= 128 && s.B <= 4096 && (c.rows != 32 || f32)) {
     // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
-    // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 63 / 70 / 78; 12 tokens of 2 sequences of 32K
-    // 62 / 74 / 85; fp32, one token of 4 sequences of 32K 225 / 226, and 249 with four times as many.  States of 64 MiB at most.
+    // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 64 / 72 / 79; 12 tokens of 2 sequences of 32K
+    // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234.  States of 64 MiB at most.
     c.want = std::max((held + s.Hkv - 1) / s.Hkv, 2 * tiles);
     c.pieces = (int)std::max(few, std::min<int64_t>({c.want, least, std::max<int64_t>((1ll << 26) / state, 1)}));
     c.units = c.want;
