@@ -430,7 +430,7 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  * same way, and so is a sequence decoded that is too short for a selection to pay.  K and V of such
  * sequences lie in pages of a pool that several sequences share:
  *
- *   lrqk_pages_append   the new tokens' rows go into their pages, in 8 bits if the pages hold 8 bits
+ *   lrqk_pages_append   the new tokens' rows go into their pages, in 8 or 4 bits if the pages hold those
  *   lrqk_chunk_attend   exact attention of the new tokens over the paged rows
  *   lrqk_pages_read     rows of the pages as dense per-head arrays: what lrqk_prefill_factorize, the
  *                       host store (K_host, V_host) and the lite rows are made from
@@ -443,7 +443,7 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  *     are left alone in the output, positions on it take no part in an attention.  Several
  *     sequences may share a page (a common prefix).  A row that is written twice at a time (by two
  *     sequences of a call, by two entries of a table with the same page, by calls that overlap) holds
- *     parts of either, in 8 bits perhaps the codes of one under the scales of the other: it is only
+ *     parts of either, in 8 or 4 bits perhaps the codes of one under the scales of the other: it is only
  *     good if both write the same.
  *   - Positions below 0 or from l_max on do not exist (the same rules).
  *   - Rows of the packed arrays before start[0] and from start[B] on belong to no sequence: what
@@ -452,16 +452,17 @@ int lrqk_prefill_factorize(const lrqk_shape* shape, const void* Q, const void* K
  * start, kv_len and table are device memory and are read by the kernels only: a captured call follows
  * what they hold when it is replayed.
  *
- * 8-bit pages: every 32 elements of a row share a scale 2^e, the smallest power of two with
- * e >= -110 for which none of them exceeds the largest code (448 for e4m3, 127 for i8), kept as the
- * byte e + 127.  Codes are x 2^-e rounded to the nearest, ties to even; since the scale is a power of
- * two that is the only rounding, and a code times its scale is exact in bf16 and fp32.  A finite
+ * 8-bit and 4-bit pages: every 32 elements of a row share a scale 2^e, the smallest power of two with
+ * e >= -110 for which none of them exceeds the largest code (448 for e4m3, 127 for i8, 6 for e2m1), kept as the
+ * byte e + 127.  The codes of e2m1 are a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 to 7 in the low three
+ * bits), two a byte: element 2 i of a row is the low half of byte i, so a row has 64 bytes.  Codes are x 2^-e rounded to the nearest, ties to even; since the scale is a power of
+ * two that is the only rounding (of e2m1 a tie goes to the even one of the eight), and a code times its scale is exact in bf16 and fp32.  A finite
  * element is read back finite: where the nearest code would mean 2^128 (bf16's largest number does) the
  * next one below is taken.  32 elements with an infinity or a NaN among them get the scale byte 255 and
  * read as NaN.  Pools that are not written by lrqk_pages_append may hold other codes and scales, -128 and the
  * NaN of e4m3 too: a product that kv_dtype does not hold is an infinity.
  */
-enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 = 3 };
+enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 = 3, LRQK_PAGE_E2M1 = 8 };
 
 /*
  *   T          rows of the packed arrays (q, out, k_new, v_new), 1 <= T < 2^24
@@ -471,7 +472,7 @@ enum { LRQK_PAGE_BF16 = 0, LRQK_PAGE_F32 = 1, LRQK_PAGE_E4M3 = 2, LRQK_PAGE_I8 =
  *   l_cap      rows allocated per head in the dense arrays of lrqk_pages_read; 0 means l_max
  *   page       positions per page: a power of two, 1 <= page <= 1024; from 16 on for prompts, whose
  *              attention takes twice as long over smaller ones
- *   n_pages    pages of the pool: at most 64 GiB of K rows and as much of V rows
+ *   n_pages    pages of the pool: at most 64 GiB of K rows and as much of V rows, without scales
  *   max_pages  entries of a sequence's row of the table, max_pages * page >= l_max
  *   kv_dtype   LRQK_KV_*: type of q, out, k_new, v_new and the dense arrays
  *   page_dtype LRQK_PAGE_*: type of the rows in the pool; BF16 and F32 need the same kv_dtype
@@ -485,9 +486,9 @@ typedef struct lrqk_pages_shape {
 
 /* All device memory, 16-byte aligned. */
 typedef struct lrqk_pages {
-  void* K;              /* page_dtype [n_pages,Hkv,page,d] */
+  void* K;              /* page_dtype [n_pages,Hkv,page,d] (e2m1: d/2 bytes a row) */
   void* V;              /* page_dtype [n_pages,Hkv,page,d] */
-  uint8_t* K_scale;     /* 8-bit pages: [n_pages,Hkv,page,d/32]; else not looked at (may be NULL) */
+  uint8_t* K_scale;     /* 8-bit and 4-bit pages: [n_pages,Hkv,page,d/32]; else not looked at (may be NULL) */
   uint8_t* V_scale;     /* likewise */
   const int32_t* table;  /* [B,max_pages] */
   const int32_t* start;  /* [B+1] */
@@ -503,7 +504,7 @@ size_t lrqk_pages_workspace_bytes(const lrqk_pages_shape* shape);
 
 /*
  * g1 — the new tokens' rows go into their pages.
- *   pages  K, V and, for 8-bit pages, K_scale, V_scale are written as described
+ *   pages  K, V and, for 8-bit and 4-bit pages, K_scale, V_scale are written as described
  *   k_new, v_new  device kv_dtype [T,Hkv,d]
  */
 int lrqk_pages_append(const lrqk_pages_shape* shape, const lrqk_pages* pages, const void* k_new,

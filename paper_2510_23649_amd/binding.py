@@ -15,7 +15,7 @@ LRQK_KV_BF16, LRQK_KV_F32 = 0, 1
 LRQK_FETCH_STAGED, LRQK_FETCH_DIRECT, LRQK_FETCH_GROUP = 0, 1, 2
 LRQK_SELECT_FRESH = 0x100
 LRQK_WS_SELECT, LRQK_WS_ATTEND, LRQK_WS_UPDATE, LRQK_WS_PREFILL = 1, 2, 3, 4
-LRQK_PAGE_BF16, LRQK_PAGE_F32, LRQK_PAGE_E4M3, LRQK_PAGE_I8 = 0, 1, 2, 3
+LRQK_PAGE_BF16, LRQK_PAGE_F32, LRQK_PAGE_E4M3, LRQK_PAGE_I8, LRQK_PAGE_E2M1 = 0, 1, 2, 3, 8
 
 
 class LrqkError(RuntimeError):
@@ -370,11 +370,12 @@ def lrqk_pages_workspace_bytes(shape: PagesShape) -> int:
     return load_library().lrqk_pages_workspace_bytes(C.byref(shape))
 
 
-_PAGE_TYPES = {torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.float8_e4m3fn}
+_PAGE_TYPES = {torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2}
 
 
 def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pages:
-    """8-bit rows may come as uint8, int8 or float8_e4m3fn: lrqk_pages_shape says what they hold."""
+    """8-bit rows may come as uint8, int8 or float8_e4m3fn, 4-bit rows (64 bytes each) as uint8 or float4_e2m1fn_x2:
+    lrqk_pages_shape says what they hold."""
     if K.dtype != V.dtype or K.dtype not in _PAGE_TYPES:
         raise TypeError(f"pages of {K.dtype} and {V.dtype}")
     p = Pages(_dev(K), _dev(V), _dev(K_scale, torch.uint8), _dev(V_scale, torch.uint8),
@@ -387,7 +388,8 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
     return p
 
 
-_PAGE_ROWS = {LRQK_PAGE_BF16: (torch.bfloat16,), LRQK_PAGE_F32: (torch.float32,)}
+_PAGE_ROWS = {LRQK_PAGE_BF16: (torch.bfloat16,), LRQK_PAGE_F32: (torch.float32,),
+              LRQK_PAGE_E2M1: (torch.uint8, torch.float4_e2m1fn_x2)}
 # what of a shape says how much its pages hold: B, Hkv and d, page to max_pages, page_dtype
 _HELD = [slice(getattr(PagesShape, a).offset, getattr(PagesShape, b).offset + 4)
          for a, b in (("B", "B"), ("Hkv", "d"), ("page", "max_pages"), ("page_dtype", "page_dtype"))]
@@ -406,13 +408,14 @@ def _hold(pages: Pages, shape: PagesShape):
     if lrqk_validate_pages(shape) != 0:
         return                               # the call says so
     K, V, K_scale, V_scale, table, start, kv_len = pages.tensors
-    eight = _PAGE_TYPES - {torch.bfloat16, torch.float32}
+    eight = (torch.uint8, torch.int8, torch.float8_e4m3fn)
     if K.dtype not in _PAGE_ROWS.get(shape.page_dtype, eight):
         raise TypeError(f"pages of {K.dtype}, page_dtype {shape.page_dtype}")
     rows = shape.n_pages * shape.Hkv * shape.page
-    need = [("K", K, rows * shape.d), ("V", V, rows * shape.d), ("table", table, shape.B * shape.max_pages),
+    row = shape.d // 2 if shape.page_dtype == LRQK_PAGE_E2M1 else shape.d
+    need = [("K", K, rows * row), ("V", V, rows * row), ("table", table, shape.B * shape.max_pages),
             ("start", start, shape.B + 1), ("kv_len", kv_len, shape.B)]
-    if shape.page_dtype not in _PAGE_ROWS:
+    if shape.page_dtype not in (LRQK_PAGE_BF16, LRQK_PAGE_F32):
         need += [("K_scale", K_scale, rows * (shape.d // 32)), ("V_scale", V_scale, rows * (shape.d // 32))]
     for name, t, n in need:
         if t is not None and t.numel() < n:  # (missing scales: the call says so)

@@ -21,7 +21,7 @@
 //   thin  at most 32 rows: each wavefront takes every fourth block of 32 positions through an LDS
 //         area of its own, without a barrier
 // The states of wavefronts that have the same rows, and of the pieces that a long context is cut into, are joined at the
-// end.  Rows of the pool's own type go straight to LDS (thin: through registers), 8-bit rows are decoded on the way into
+// end.  Rows of the pool's own type go straight to LDS (thin: through registers), codes are decoded on the way into
 // it, exactly: a code times its scale is a bf16 number.
 //
 // V rows that a token does not see meet its weights as 0 * V, which is not 0 if V is not finite.
@@ -229,8 +229,9 @@ __device__ __forceinline__ int v_chunk(int row, int c) { return row * kRowB<true
 // and a lane's part of an address does not change from block to block.  SMALL: smaller pages, a table entry for every row.
 template <bool BF16, int PAGE, int ROWS, int NW, bool SMALL = false>
 struct Block {
-  static constexpr int kRow16 = kD * page_elem_bytes(PAGE) / 16;          // 16-byte chunks of a row in the pool
-  static constexpr int kLanes = kRow16;                                   // lanes a row: 16 bytes each
+  static constexpr int kRow16 = row_bytes(PAGE) / 16;                     // 16-byte chunks of a row in the pool
+  using Raw = std::conditional_t<PAGE == LRQK_PAGE_E2M1 && !BF16, uint2, uint4>;  // what a lane loads of a row
+  static constexpr int kLanes = row_bytes(PAGE) / (int)sizeof(Raw);       // lanes a row
   static constexpr int kPass = 64 / kLanes;                               // rows a load of the wavefront
   static constexpr int kMine = ROWS / NW;                                 // rows of the wavefront
   static constexpr int kN = kMine / kPass;                                // such loads
@@ -245,7 +246,7 @@ struct Block {
     uint32_t there;           // bit of each row
   };
   struct Held {
-    uint4 x[kN];
+    Raw x[kN];
     uint32_t scale[kN];
   };
   int pg[kGroups];  // the groups' pages, one block ahead
@@ -307,18 +308,19 @@ struct Block {
       find_rows(a, b, kvh, f.p0, end, lane, at);
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        r.x[i] = static_cast<const uint4*>(base)[(size_t)(at[i] + c)];
-        if constexpr (is8(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) >> 1)];
+        r.x[i] = static_cast<const Raw*>(base)[(size_t)at[i] * (kLanes / kRow16) + c];
+        if constexpr (coded(PAGE)) r.scale[i] = scale[(size_t)(at[i] / (kRow16 / kScales)) + c * kScales / kLanes];
       }
     } else {
       // first what all lanes share, then what a lane adds in every block, then a number that the instruction holds
-      const uint32_t mine = (uint32_t)(lane / kLanes * kRow16 + c);
+      const uint32_t mine = (uint32_t)lane;  // lane / kLanes * kLanes + c
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const int g = i * kPass / kGroup, rows = i * kPass - g * kGroup;
-        r.x[i] = (static_cast<const uint4*>(base) + (size_t)f.place[g])[mine + rows * kRow16];
-        // 16 codes are half a scale block; a row has 8 chunks and 4 scales
-        if constexpr (is8(PAGE)) r.scale[i] = (scale + ((size_t)f.place[g] >> 1))[(mine >> 1) + rows * kScales];
+        r.x[i] = (static_cast<const Raw*>(base) + (size_t)f.place[g] * (kLanes / kRow16))[mine + rows * kLanes];
+        // (kRow16 chunks of a row and kScales scales: a lane's codes are one scale block or half of one)
+        if constexpr (coded(PAGE))
+          r.scale[i] = (scale + (size_t)(f.place[g] / (kRow16 / kScales)))[mine * kScales / kLanes + rows * kScales];
       }
     }
   }
@@ -342,9 +344,28 @@ struct Block {
     }
   }
 
-  static __device__ __forceinline__ void widen(const uint4 x, uint32_t byte, uint4 (&o)[kOut]) {
-    if constexpr (!is8(PAGE)) {
+  // Codes as they go into LDS, in chunks; `swap`: chunks j and j ^ 2 change places.  A lane that decodes 32 codes of e2m1 stores
+  // four chunks, and two rows' lanes would meet in the same banks: in every other row it begins with the third.
+  static constexpr bool kSwaps = BF16 && PAGE == LRQK_PAGE_E2M1;
+  static __device__ __forceinline__ int chunk_at(int c, int j, bool swap) { return c + (kSwaps && swap ? j ^ 2 : j); }
+  static __device__ __forceinline__ void widen(const Raw x, uint32_t byte, bool swap, uint4 (&o)[kOut]) {
+    if constexpr (!coded(PAGE)) {
       o[0] = x;
+    } else if constexpr (PAGE == LRQK_PAGE_E2M1) {
+      const float s = scale_of(byte);
+      if constexpr (BF16) {
+        const uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = decode8_bf16<PAGE>(w[j], s);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float f[8];
+          decode8<PAGE>(j ? x.y : x.x, s, f);
+          o[2 * j] = __builtin_bit_cast(uint4, f32x4{f[0], f[1], f[2], f[3]});
+          o[2 * j + 1] = __builtin_bit_cast(uint4, f32x4{f[4], f[5], f[6], f[7]});
+        }
+      }
     } else {
       const float s = scale_of(byte);
       const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -367,10 +388,11 @@ struct Block {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int row = w * kMine + row_in_wave(i, lane), c = (lane % kLanes) * kOut;
+      const bool swap = row & 1;
       uint4 o[kOut];
-      widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
+      widen(r.x[i], coded(PAGE) ? r.scale[i] : 0u, swap, o);
 #pragma unroll
-      for (int j = 0; j < kOut; ++j) *reinterpret_cast<uint4*>(kt + k_chunk<BF16>(row, c + j)) = o[j];
+      for (int j = 0; j < kOut; ++j) *reinterpret_cast<uint4*>(kt + k_chunk<BF16>(row, chunk_at(c, j, swap))) = o[j];
     }
   }
 
@@ -381,8 +403,9 @@ struct Block {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int in_wave = row_in_wave(i, lane), row = w * kMine + in_wave, c = (lane % kLanes) * kOut;
+      const bool swap = row & 1;
       uint4 o[kOut];
-      widen(r.x[i], is8(PAGE) ? r.scale[i] : 0u, o);
+      widen(r.x[i], coded(PAGE) ? r.scale[i] : 0u, swap, o);
       if (there != kAll && !((there >> in_wave) & 1)) {
 #pragma unroll
         for (int j = 0; j < kOut; ++j) o[j] = make_uint4(0, 0, 0, 0);
@@ -396,7 +419,7 @@ struct Block {
       }
 #pragma unroll
       for (int j = 0; j < kOut; ++j)
-        *reinterpret_cast<uint4*>(vt + (BF16 ? v_chunk(row, c + j) : row * kRowB<false> + ((c + j) << 4))) = o[j];
+        *reinterpret_cast<uint4*>(vt + (BF16 ? v_chunk(row, chunk_at(c, j, swap)) : row * kRowB<false> + ((c + j) << 4))) = o[j];
     }
     return left_out;
   }
@@ -692,8 +715,10 @@ __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows,
       const int64_t at = row_of(a.m, p.b, kvh, pos);
       if (at < 0) continue;
       float v;
-      if constexpr (is8(PAGE)) {  // as Block::widen makes it: a pool from elsewhere may hold what exceeds the type
-        const uint2 code = make_uint2(static_cast<const uint8_t*>(a.V)[at * kD + d], 0u);
+      if constexpr (coded(PAGE)) {  // as Block::widen makes it: a pool from elsewhere may hold what exceeds the type
+        Codes8<PAGE> code;
+        if constexpr (PAGE == LRQK_PAGE_E2M1) code = static_cast<const uint8_t*>(a.V)[(at * kD + d) >> 1] >> (d & 1) * 4;
+        else code = make_uint2(static_cast<const uint8_t*>(a.V)[at * kD + d], 0u);
         const float scale = scale_of(a.V_scale[at * kScales + d / kScaleBlock]);
         if constexpr (BF16) {
           v = __uint_as_float(decode8_bf16<PAGE>(code, scale).x << 16);
@@ -756,14 +781,14 @@ struct TileLoop {
   __device__ __forceinline__ void fetch_k(int i, char* kt) {
     const int p0 = from + i * BN + w * B::kMine;
     blk.find(a, p.b, kvh, p0, end, lane, fk);
-    if constexpr (is8(PAGE)) B::load(a, p.b, kvh, end, a.K, a.K_scale, fk, lane, hk);
+    if constexpr (coded(PAGE)) B::load(a, p.b, kvh, end, a.K, a.K_scale, fk, lane, hk);
     else B::template load_direct<false>(a.K, fk, w, lane, kt);
     if (lane == 0) there[i & 3][w] = (uint16_t)fk.there;
     blk.look_up(a.m, p.b, p0 + BN, end);
   }
   // of V, found before
   __device__ __forceinline__ void fetch_v(int i, char* vt) {
-    if constexpr (is8(PAGE)) {
+    if constexpr (coded(PAGE)) {
       B::load(a, p.b, kvh, end, a.V, a.V_scale, fv, lane, hv);
     } else {
       const bool part = from + (i + 1) * BN > least;
@@ -777,7 +802,7 @@ struct TileLoop {
   }
   // what came through registers goes into LDS; all that this wavefront has fetched is there
   __device__ __forceinline__ void arrive(bool k, char* kt, int i_v, char* vt) {
-    if constexpr (is8(PAGE)) {
+    if constexpr (coded(PAGE)) {
       if (k) B::store_k(hk, w, lane, kt);
       cleared |= B::store_v(hv, fv.there, from + (i_v + 1) * BN > least, w, lane, vt);
     } else {
@@ -811,11 +836,11 @@ struct TileLoop {
     const int n = (end - from + BN - 1) / BN;
     blk.look_up(a.m, p.b, from + w * B::kMine, end);
     fetch_k(0, kt0);
-    if constexpr (is8(PAGE)) B::store_k(hk, w, lane, kt0);
+    if constexpr (coded(PAGE)) B::store_k(hk, w, lane, kt0);
     fv = fk;
     if (n > 1) fetch_k(1, kt1);
     fetch_v(0, vt0);
-    if constexpr (!is8(PAGE)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!coded(PAGE)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (busy) {
       f32x16 first = r.scores(kt0, lane);
@@ -869,7 +894,7 @@ struct PlainLoop {
     const int mine = p0 + w * B::kMine;
     blk.find(a, p.b, kvh, mine, end, lane, x.f);
     blk.look_up(a.m, p.b, mine + BN, end);
-    if constexpr (is8(PAGE)) {
+    if constexpr (coded(PAGE)) {
       B::load(a, p.b, kvh, end, a.K, a.K_scale, x.f, lane, x.hk);
       B::load(a, p.b, kvh, end, a.V, a.V_scale, x.f, lane, x.hv);
     } else {
@@ -886,14 +911,14 @@ struct PlainLoop {
   }
   // The block at p0; the next one is on its way, or, with 8-bit rows, the one after the next.
   __device__ __forceinline__ void round(int p0, Way& now, Way& other) {
-    if constexpr (is8(PAGE)) {
+    if constexpr (coded(PAGE)) {
       B::store_k(now.hk, w, lane, now.k);
       cleared |= B::store_v(now.hv, now.f.there, p0 + BN > least, w, lane, now.v);
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     __syncthreads();
-    if constexpr (is8(PAGE)) {
+    if constexpr (coded(PAGE)) {
       if (p0 + 2 * BN < end) fetch(p0 + 2 * BN, now);
     } else {
       if (p0 + BN < end) fetch(p0 + BN, other);
@@ -907,7 +932,7 @@ struct PlainLoop {
     Way x{kt0, vt0, {}, {}, {}}, y{kt1, vt1, {}, {}, {}};
     blk.look_up(a.m, p.b, from + w * B::kMine, end);
     fetch(from, x);
-    if (is8(PAGE) && from + BN < end) fetch(from + BN, y);
+    if (coded(PAGE) && from + BN < end) fetch(from + BN, y);
     for (int p0 = from; p0 < end; p0 += 2 * BN) {
       round(p0, x, y);
       if (p0 + BN < end) round(p0 + BN, y, x);
@@ -1313,7 +1338,7 @@ LRQK_API int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* 
   const Args a{make_map(s, *pg), pg->K, pg->V, pg->K_scale, pg->V_scale, q, out,
                c.pieces > 1 ? static_cast<float*>(workspace) : nullptr, s.Hq / s.Hkv,
                __builtin_ctz((unsigned)c.rows), c.pieces, c.prefer, c.want, c.least,
-               (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(kD * page_elem_bytes(s.page_dtype) / 16), s.scale};
+               (uint32_t)s.Hkv * (uint32_t)s.page * (uint32_t)(row_bytes(s.page_dtype) / 16), s.scale};
   hipError_t e = hipSuccess;
   by_type(s, [&](auto bf16, auto page) {
     e = launch<bf16.value, page.value>(s, c, a, static_cast<hipStream_t>(stream));

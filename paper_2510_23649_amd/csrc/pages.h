@@ -1,4 +1,4 @@
-// Device helpers of the paged K/V cache: where a position lies, and rows held in 8 bits.
+// Device helpers of the paged K/V cache: where a position lies, and rows held in 8 or 4 bits.
 #pragma once
 
 #include <type_traits>
@@ -18,12 +18,16 @@ constexpr int kScaleBlock = 32;               // elements of a row that share a 
 constexpr int kScales = kD / kScaleBlock;     // scale bytes of a row
 constexpr int kMinExp = -110;                 // smallest scale 2^e (include/lrqk.h)
 
-__host__ __device__ constexpr bool is8(int page_dtype) {
-  return page_dtype == LRQK_PAGE_E4M3 || page_dtype == LRQK_PAGE_I8;
+// Rows are codes with scales (8 or 4 bits).
+__host__ __device__ constexpr bool coded(int page_dtype) {
+  return page_dtype == LRQK_PAGE_E4M3 || page_dtype == LRQK_PAGE_I8 || page_dtype == LRQK_PAGE_E2M1;
 }
-__host__ __device__ constexpr int page_elem_bytes(int page_dtype) {
-  return page_dtype == LRQK_PAGE_F32 ? 4 : page_dtype == LRQK_PAGE_BF16 ? 2 : 1;
+__host__ __device__ constexpr int row_bytes(int page_dtype) {
+  return kD * (page_dtype == LRQK_PAGE_F32 ? 32 : page_dtype == LRQK_PAGE_BF16 ? 16 : page_dtype == LRQK_PAGE_E2M1 ? 4 : 8) / 8;
 }
+// Eight consecutive elements of a row as codes: element 2 i of e2m1 is the low half of byte i.
+template <int PAGE>
+using Codes8 = std::conditional_t<PAGE == LRQK_PAGE_E2M1, uint32_t, uint2>;
 
 // The shape and the tables as the kernels take them.
 struct Map {
@@ -62,22 +66,34 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7fc00000u : x);
 }
 
-// Eight codes (two dwords) times their scale, in fp32 (exact).
+// Eight codes times their scale, in fp32 (exact).
 template <int PAGE>
-__device__ __forceinline__ void decode8(uint2 c, float s, float (&x)[8]) {
+__device__ __forceinline__ void decode8(Codes8<PAGE> c, float s, float (&x)[8]) {
+  if constexpr (PAGE == LRQK_PAGE_E2M1) {
+    auto pair = [&](auto i) {
+      const auto y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, i.value);
+      x[2 * i.value] = y[0] * s;
+      x[2 * i.value + 1] = y[1] * s;
+    };
+    pair(std::integral_constant<int, 0>{});
+    pair(std::integral_constant<int, 1>{});
+    pair(std::integral_constant<int, 2>{});
+    pair(std::integral_constant<int, 3>{});
+  } else {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t w = i ? c.y : c.x;
-    if constexpr (PAGE == LRQK_PAGE_E4M3) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
-      const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-      x[4 * i] = lo[0] * s;
-      x[4 * i + 1] = lo[1] * s;
-      x[4 * i + 2] = hi[0] * s;
-      x[4 * i + 3] = hi[1] * s;
-    } else {
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w = i ? c.y : c.x;
+      if constexpr (PAGE == LRQK_PAGE_E4M3) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        x[4 * i] = lo[0] * s;
+        x[4 * i + 1] = lo[1] * s;
+        x[4 * i + 2] = hi[0] * s;
+        x[4 * i + 3] = hi[1] * s;
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = (float)(int8_t)(w >> (8 * j)) * s;
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = (float)(int8_t)(w >> (8 * j)) * s;
+      }
     }
   }
 }
@@ -85,8 +101,15 @@ __device__ __forceinline__ void decode8(uint2 c, float s, float (&x)[8]) {
 // The same as four packed bf16 pairs: exact too (a code has at most seven bits, and with scales as they are written the product
 // is a normal number of bf16 or 0; with larger ones, in a pool from elsewhere, it may be an infinity).
 template <int PAGE>
-__device__ __forceinline__ uint4 decode8_bf16(uint2 c, float s) {
-  if constexpr (PAGE == LRQK_PAGE_E4M3) {
+__device__ __forceinline__ uint4 decode8_bf16(Codes8<PAGE> c, float s) {
+  using std::integral_constant;
+  if constexpr (PAGE == LRQK_PAGE_E2M1) {
+    auto pair = [&](auto i) {
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, i.value));
+    };
+    return make_uint4(pair(integral_constant<int, 0>{}), pair(integral_constant<int, 1>{}), pair(integral_constant<int, 2>{}),
+                      pair(integral_constant<int, 3>{}));
+  } else if constexpr (PAGE == LRQK_PAGE_E4M3) {
     auto pair = [&](uint32_t w, auto high) {
       return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, high.value));
     };
@@ -102,12 +125,12 @@ __device__ __forceinline__ uint4 decode8_bf16(uint2 c, float s) {
 }
 
 // The scale byte of a block whose largest magnitude has the bits `top` (compared as integers, so that
-// infinity and NaN win): the smallest e >= kMinExp with max <= 448 2^e or 127 2^e.  448 = 1.75 * 2^8,
-// 127 = 1.984375 * 2^6: one more where the mantissa is above theirs.
+// infinity and NaN win): the smallest e >= kMinExp with max <= 448 2^e, 127 2^e or 6 2^e.  448 = 1.75 * 2^8,
+// 127 = 1.984375 * 2^6, 6 = 1.5 * 2^2: one more where the mantissa is above theirs.
 template <int PAGE>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-  constexpr int kTopExp = PAGE == LRQK_PAGE_E4M3 ? 8 : 6;
-  constexpr uint32_t kTopMant = PAGE == LRQK_PAGE_E4M3 ? 0x600000u : 0x7e0000u;
+  constexpr int kTopExp = PAGE == LRQK_PAGE_E4M3 ? 8 : PAGE == LRQK_PAGE_I8 ? 6 : 2;
+  constexpr uint32_t kTopMant = PAGE == LRQK_PAGE_E4M3 ? 0x600000u : PAGE == LRQK_PAGE_I8 ? 0x7e0000u : 0x400000u;
   const int ex = (int)(top >> 23);
   if (ex == 255) return 255u;
   const int e = ex - 127 - kTopExp + ((top & 0x7fffffu) > kTopMant ? 1 : 0);
@@ -115,31 +138,40 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 }
 
 // Eight elements as codes of a block with that scale byte.  With the largest scale (that of a block whose largest magnitude is
-// above 448 2^119 or 127 2^121) a number may lie nearest to 256 2^120 or 64 2^122, which is 2^128: it takes the code below, so
-// that what is finite is read back finite.
+// above 448 2^119, 127 2^121 or 6 2^125) a number may lie nearest to 256 2^120, 64 2^122 or 4 2^126, which is 2^128: it takes the
+// code below, so that what is finite is read back finite.
 template <int PAGE>
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], uint32_t byte) {
-  if (byte == 255u) return make_uint2(0u, 0u);
+__device__ __forceinline__ Codes8<PAGE> encode8(const float (&x)[8], uint32_t byte) {
+  if (byte == 255u) return Codes8<PAGE>{};
   const float inv = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte), a normal number
-  constexpr bool kE4m3 = PAGE == LRQK_PAGE_E4M3;
-  const float most = byte >= (kE4m3 ? 247u : 249u) ? (kE4m3 ? 240.0f : 63.0f) : (kE4m3 ? 448.0f : 127.0f);
+  constexpr uint32_t kLast = PAGE == LRQK_PAGE_E4M3 ? 247u : PAGE == LRQK_PAGE_I8 ? 249u : 253u;
+  constexpr float kTop = PAGE == LRQK_PAGE_E4M3 ? 448.0f : PAGE == LRQK_PAGE_I8 ? 127.0f : 6.0f;
+  constexpr float kBelow = PAGE == LRQK_PAGE_E4M3 ? 240.0f : PAGE == LRQK_PAGE_I8 ? 63.0f : 3.0f;
+  const float most = byte >= kLast ? kBelow : kTop;
   auto scaled = [&](int i) { return __builtin_amdgcn_fmed3f(x[i] * inv, -most, most); };
-  uint32_t w[2];
+  if constexpr (PAGE == LRQK_PAGE_E2M1) {
+    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, scaled(0), scaled(1), 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, scaled(2), scaled(3), 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, scaled(4), scaled(5), 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, scaled(6), scaled(7), 1.0f, 3);
+  } else {
+    uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if constexpr (PAGE == LRQK_PAGE_E4M3) {
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i), scaled(4 * i + 1), 0, false);
-      v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i + 2), scaled(4 * i + 3), v, true);
-      w[i] = (uint32_t)v;
-    } else {
-      uint32_t v = 0;
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (PAGE == LRQK_PAGE_E4M3) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i), scaled(4 * i + 1), 0, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(4 * i + 2), scaled(4 * i + 3), v, true);
+        w[i] = (uint32_t)v;
+      } else {
+        uint32_t v = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        v |= ((uint32_t)(int)__builtin_rintf(scaled(4 * i + j)) & 0xffu) << (8 * j);
-      w[i] = v;
+        for (int j = 0; j < 4; ++j)
+          v |= ((uint32_t)(int)__builtin_rintf(scaled(4 * i + j)) & 0xffu) << (8 * j);
+        w[i] = v;
+      }
     }
+    return make_uint2(w[0], w[1]);
   }
-  return make_uint2(w[0], w[1]);
 }
 
 // Sequence that each packed row t belongs to, or -1; the whole wavefront asks, each lane for its own rows: the starts are
@@ -168,7 +200,7 @@ __device__ __forceinline__ int sequence_of(const Map& m, int t) {
   return b[0];
 }
 
-// f(bf16 dense rows, page type) for the five combinations that check_pages lets through
+// f(bf16 dense rows, page type) for the combinations that check_pages lets through
 template <typename F>
 void by_type(const lrqk_pages_shape& s, F f) {
   using std::integral_constant;
@@ -183,7 +215,8 @@ void by_type(const lrqk_pages_shape& s, F f) {
     case LRQK_PAGE_BF16: with(integral_constant<int, LRQK_PAGE_BF16>{}); break;
     case LRQK_PAGE_F32: with(integral_constant<int, LRQK_PAGE_F32>{}); break;
     case LRQK_PAGE_E4M3: with(integral_constant<int, LRQK_PAGE_E4M3>{}); break;
-    default: with(integral_constant<int, LRQK_PAGE_I8>{}); break;
+    case LRQK_PAGE_I8: with(integral_constant<int, LRQK_PAGE_I8>{}); break;
+    default: with(integral_constant<int, LRQK_PAGE_E2M1>{}); break;
   }
 }
 

@@ -11,7 +11,7 @@ namespace lrqk {
 int check_pages(const lrqk_pages_shape* s) {
   if (!s) return LRQK_EINVAL;
   if (s->kv_dtype != LRQK_KV_BF16 && s->kv_dtype != LRQK_KV_F32) return LRQK_EINVAL;
-  if (s->page_dtype < LRQK_PAGE_BF16 || s->page_dtype > LRQK_PAGE_I8) return LRQK_EINVAL;
+  if ((s->page_dtype < LRQK_PAGE_BF16 || s->page_dtype > LRQK_PAGE_I8) && s->page_dtype != LRQK_PAGE_E2M1) return LRQK_EINVAL;
   if (s->page_dtype == LRQK_PAGE_BF16 && s->kv_dtype != LRQK_KV_BF16) return LRQK_EINVAL;
   if (s->page_dtype == LRQK_PAGE_F32 && s->kv_dtype != LRQK_KV_F32) return LRQK_EINVAL;
   if (s->B < 1 || s->Hq < 1 || s->Hkv < 1 || s->n_max < 1 || s->n_pages < 1) return LRQK_ESHAPE;
@@ -25,7 +25,7 @@ int check_pages(const lrqk_pages_shape* s) {
   if (s->max_pages < 1 || (int64_t)s->max_pages * s->page < s->l_max) return LRQK_ESHAPE;
   if (!std::isfinite(s->scale)) return LRQK_ESHAPE;
   // 16-byte chunks of a pool are counted in 32 bits
-  const int64_t page16 = (int64_t)s->Hkv * s->page * (kD * pages::page_elem_bytes(s->page_dtype) / 16);
+  const int64_t page16 = (int64_t)s->Hkv * s->page * (pages::row_bytes(s->page_dtype) / 16);
   if (page16 * s->n_pages > (int64_t)1 << 32) return LRQK_ESHAPE;
   return LRQK_OK;
 }
@@ -33,7 +33,7 @@ int check_pages(const lrqk_pages_shape* s) {
 bool pages_given(const lrqk_pages_shape& s, const lrqk_pages* p) {
   if (!p) return false;
   auto ok = [](const void* x) { return x && aligned16(x); };
-  if (pages::is8(s.page_dtype) && (!ok(p->K_scale) || !ok(p->V_scale))) return false;
+  if (pages::coded(s.page_dtype) && (!ok(p->K_scale) || !ok(p->V_scale))) return false;
   return ok(p->K) && ok(p->V) && ok(p->table) && ok(p->start) && ok(p->kv_len);
 }
 
@@ -69,7 +69,7 @@ __device__ __forceinline__ void get8(uint4 a, uint4 b, float (&x)[8]) {
 }
 
 // A 16-lane group takes rows of k_new and v_new, 8 elements a lane; the rows are on their way while their places are found.
-// An 8-bit row has its four blocks of 32 elements in four lanes each: a block's largest magnitude takes two DPP steps.
+// A row of codes has its four blocks of 32 elements in four lanes each: a block's largest magnitude takes two DPP steps.
 // Bound by memory: 4 prompts of up to 8192 tokens, bf16 to e4m3 (K and V, 99 MB), 22 us.  One
 // token of 16 sequences is 5 us of loads that wait for each other (start, then length and table, then the row's place).
 template <bool BF16, int PAGE>
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kMoveThreads) void pages_append_kernel(const Map m,
       if (t[j] < q.first || t[j] >= q.first + q.n || p < 0 || p >= m.l_max) continue;
       const int64_t row = row_of(m, b[j], (int)((uint32_t)r % (uint32_t)m.Hkv), p);
       if (row < 0) continue;
-      if constexpr (!is8(PAGE)) {
+      if constexpr (!coded(PAGE)) {
         store8<BF16>(K, row, c, k[j], k2[j]);
         store8<BF16>(V, row, c, v[j], v2[j]);
       } else {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kMoveThreads) void pages_append_kernel(const Map m,
           top = max(top, dev::dpp_u32<0xB1>(top));  // over the four lanes of a block
           top = max(top, dev::dpp_u32<0x4E>(top));
           const uint32_t byte = scale_byte<PAGE>(top);
-          static_cast<uint2*>(which ? V : K)[row * 16 + c] = encode8<PAGE>(x, byte);
+          static_cast<Codes8<PAGE>*>(which ? V : K)[row * 16 + c] = encode8<PAGE>(x, byte);
           if ((c & 3) == 0) (which ? V_scale : K_scale)[row * kScales + (c >> 2)] = (uint8_t)byte;
         }
       }
@@ -136,7 +136,9 @@ __global__ __launch_bounds__(kMoveThreads) void pages_read_kernel(const Map m, c
                                                                   int stretches, int64_t units, int lrows,
                                                                   void* K_out, void* V_out) {
   constexpr int kLanes = kD * (BF16 ? 2 : 4) / 16, kPass = kMoveThreads / kLanes, kN = kReadSpan / kPass;
-  using Raw = std::conditional_t<!is8(PAGE), uint4, std::conditional_t<BF16, uint2, uint32_t>>;
+  constexpr bool k4 = PAGE == LRQK_PAGE_E2M1;
+  using Raw = std::conditional_t<!coded(PAGE), uint4,
+                                 std::conditional_t<BF16, Codes8<PAGE>, std::conditional_t<k4, uint16_t, uint32_t>>>;
   const int grp = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int kvh = (int)(u % m.Hkv);
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(kMoveThreads) void pages_read_kernel(const Map m, c
       for (int i = 0; i < kN; ++i) {
         if (row[i] < 0) continue;
         x[which][i] = static_cast<const Raw*>(which ? V : K)[row[i] * kLanes + c];
-        if constexpr (is8(PAGE)) sc[which][i] = (which ? V_scale : K_scale)[row[i] * kScales + c / (kLanes / kScales)];
+        if constexpr (coded(PAGE)) sc[which][i] = (which ? V_scale : K_scale)[row[i] * kScales + c / (kLanes / kScales)];
       }
     }
 #pragma unroll
@@ -171,13 +173,14 @@ __global__ __launch_bounds__(kMoveThreads) void pages_read_kernel(const Map m, c
       for (int i = 0; i < kN; ++i) {
         if (row[i] < 0) continue;
         uint4 y;
-        if constexpr (!is8(PAGE)) {
+        if constexpr (!coded(PAGE)) {
           y = x[which][i];
         } else if constexpr (BF16) {
           y = decode8_bf16<PAGE>(x[which][i], scale_of(sc[which][i]));
         } else {
           float f[8];
-          decode8<PAGE>(make_uint2(x[which][i], 0u), scale_of(sc[which][i]), f);
+          if constexpr (k4) decode8<PAGE>((uint32_t)x[which][i], scale_of(sc[which][i]), f);
+          else decode8<PAGE>(make_uint2(x[which][i], 0u), scale_of(sc[which][i]), f);
           y = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
         }
         const dev::u32x4 z = {y.x, y.y, y.z, y.w};
