@@ -540,6 +540,156 @@ int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* pages, co
                       void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * Rotary positions.  Of a row of d elements the first `rot` are turned in pairs by angles that grow with
+ * the token's position, the others stay as they are:
+ *   pair j of rot/2 at position p:  a = 2 pi frac(p turns[j] / 2^64),
+ *   y_u = amplitude (x_u cos a - x_v sin a),   y_v = amplitude (x_v cos a + x_u sin a)
+ *   LRQK_ROPE_HALVES  u = j, v = j + rot/2;     LRQK_ROPE_PAIRS  u = 2 j, v = 2 j + 1
+ * The fraction is exact for every position (an integer product mod 2^64): far positions lose nothing.  Sums are
+ * fp32; a result is off by at most 8 2^-24 amplitude (|x_u| + |x_v|), and the rounding to its type.
+ *   rot        even, 2 <= rot <= d
+ *   back       0, or 1: by -a, the transposed map: what turns gradients back (and, up to amplitude^2, undoes it)
+ *   amplitude  finite
+ *   turns      device, [rot/2], as written by lrqk_rope_turns (copied to the device by the caller)
+ */
+enum { LRQK_ROPE_HALVES = 0, LRQK_ROPE_PAIRS = 1 };
+typedef struct lrqk_rope {
+  int32_t layout, rot, back;
+  float amplitude;
+  const uint64_t* turns;
+} lrqk_rope;
+
+/*
+ * r0 -- the table of a rope: turns[j] = f_j / (2 pi) in units of 2^-64 turns, f_j radians a position.
+ * Host only.  F_j = base^(-2 j / rot), and
+ *   LRQK_ROPE_PLAIN   f = F
+ *   LRQK_ROPE_LINEAR  f = F / factor
+ *   LRQK_ROPE_BASE    f = F with base factor^(rot / (rot - 2)) for base (rot = 2: base)
+ *   LRQK_ROPE_BANDS   f = F (s + (1 - s) / factor), s = (l_orig F / (2 pi) - low) / (high - low) within [0, 1]:
+ *                     pairs that turn more than `high` times in the original length l_orig stay, those that turn less
+ *                     than `low` times are stretched
+ *   LRQK_ROPE_RAMP    the same with s = 1 - (j - j0) / max(j1 - j0, 0.001) within [0, 1], linear in j from the pair that
+ *                     turns `high` times to the one that turns `low` times: j(n) = rot ln(l_orig / (2 pi n)) / (2 ln base),
+ *                     j0 = max(floor(j(high)), 0), j1 = min(ceil(j(low)), rot/2 - 1)
+ *   base      > 1;  factor > 0 (not looked at by PLAIN);  0 < low < high and l_orig >= 1 (BANDS and RAMP)
+ *   turns      host, [rot/2]  written
+ *   amplitude  host, may be NULL: written with 0.1 ln(factor) + 1 for RAMP (factor >= 1), 1 otherwise
+ */
+enum { LRQK_ROPE_PLAIN = 0, LRQK_ROPE_LINEAR = 1, LRQK_ROPE_BASE = 2, LRQK_ROPE_BANDS = 3, LRQK_ROPE_RAMP = 4 };
+int lrqk_rope_turns(int32_t rot, int32_t scaling, double base, double factor, double low, double high,
+                    int32_t l_orig, uint64_t* turns, float* amplitude);
+
+/*
+ *   T                 tokens, 1 <= T < 2^24
+ *   Hq, Hkv           heads of q and of k, 1 to 1024 each (that of an array that is not given is not looked at)
+ *   q_type, q_out_type, k_type   LRQK_KV_*; k_out has the type of k
+ *   q_stride, ...     elements from one token's rows to the next: 0 for dense rows (heads * d), else at least that
+ *                     and a multiple of 16 bytes; so q and k may be parts of one projection's rows
+ *   d = 128
+ */
+typedef struct lrqk_rotate_shape {
+  int32_t T, Hq, Hkv, d;
+  int32_t q_type, q_out_type, k_type;
+  int32_t q_stride, q_out_stride, k_stride, k_out_stride;
+} lrqk_rotate_shape;
+
+/*
+ * r1 -- queries and keys at positions of their own: what lrqk_factor_update, lrqk_append_token and
+ * lrqk_decode_step take (q in fp32, k in kv_dtype), lrqk_chunk_attend and lrqk_pages_append; with rope->back their
+ * gradients.
+ *   pos        device int32 [T], any value
+ *   q, q_out   device [T,Hq,d]    both or neither
+ *   k, k_out   device [T,Hkv,d]   both or neither; one of q and k at least
+ * In place if an output is its input, with the same type and stride; else they must not overlap.
+ */
+int lrqk_rotate(const lrqk_rotate_shape* shape, const lrqk_rope* rope, const int32_t* pos, const void* q,
+                void* q_out, const void* k, void* k_out, void* stream);
+
+/*
+ * Rows of new tokens as a projection leaves them (lrqk_pages_rotate_append).
+ *   q, k, v    device kv_dtype [T,Hq,d], [T,Hkv,d], [T,Hkv,d]; q may be NULL
+ *   *_stride   as in lrqk_rotate_shape
+ *   q_out      device kv_dtype [T,Hq,d], dense; NULL exactly if q is.  May be q where that is dense; must not overlap
+ *              k, v or, else, q
+ *   pos, slot  device int32 [T], both or neither: each row's position and the row of the pool it goes to, as
+ *              written by lrqk_pages_advance.  Then start, kv_len and table are not looked at
+ */
+typedef struct lrqk_new_rows {
+  const void *q, *k, *v;
+  int32_t q_stride, k_stride, v_stride;
+  void* q_out;
+  const int32_t *pos, *slot;
+} lrqk_new_rows;
+
+/*
+ * g4 -- a layer's new rows in one call: q_out is q turned; k, turned and rounded to kv_dtype, and v go into their pages as by
+ * lrqk_pages_append.  The same bits as lrqk_rotate and lrqk_pages_append give.
+ * A token at a position below 0 does not exist: nothing of it is written, q_out included.  One at l_max or beyond, or
+ * without a page (a slot outside [0, n_pages * page)), has its q turned, its k and v are dropped.
+ */
+int lrqk_pages_rotate_append(const lrqk_pages_shape* shape, const lrqk_pages* pages, const lrqk_rope* rope,
+                             const lrqk_new_rows* rows, void* stream);
+
+/*
+ * Tables of a paged cache that live on the device: what the calls above read, made from how many tokens each
+ * request keeps and gets.  All device memory, 16-byte aligned.
+ *   refs     how many table entries name a page; 0 (or less): it is free.  lrqk_pages_advance counts what it takes and gives
+ *            back.  A caller that lets several sequences share a page, or keeps one for itself, counts that too
+ *   table    sequence b holds the pages of its kv_len[b] positions in its first ceil(kv_len[b] / page) entries
+ *   status   per sequence: LRQK_ADVANCE_*
+ *   seq, pos, slot   per packed row: its sequence, its position, and the row of the pool (page * table[b][pos / page] +
+ *            pos mod page); -1 for rows that belong to no sequence.  Each may be NULL
+ */
+typedef struct lrqk_pages_tables {
+  int32_t* refs;    /* [n_pages]      read and updated */
+  int32_t* table;   /* [B,max_pages]  read and updated */
+  int32_t* kv_len;  /* [B]            read and updated */
+  int32_t* start;   /* [B+1]          written */
+  int32_t* status;  /* [B]            written */
+  int32_t* seq;     /* [T]            written */
+  int32_t* pos;     /* [T]            written */
+  int32_t* slot;    /* [T]            written */
+} lrqk_pages_tables;
+
+enum {
+  LRQK_ADVANCE_OK = 0,
+  LRQK_ADVANCE_LONG = 1,   /* more than n_max new tokens, or than l_max positions                     */
+  LRQK_ADVANCE_SHARED = 2, /* its next row lies on a page that is counted more than once              */
+  LRQK_ADVANCE_PAGES = 3,  /* not enough free pages for it and those before it                        */
+  LRQK_ADVANCE_ROWS = 4    /* more than T rows, its and those of the sequences before it               */
+};
+
+/* An empty cache: refs and kv_len 0, table -1. */
+int lrqk_pages_tables_init(const lrqk_pages_shape* shape, const lrqk_pages_tables* tables, void* stream);
+
+/* Bytes of device workspace lrqk_pages_advance needs for this shape (0 on a bad shape). */
+size_t lrqk_pages_advance_workspace_bytes(const lrqk_pages_shape* shape);
+
+/*
+ * g5 -- the tables of a step from those of the step before.  Sequence b is cut back to its first keep[b] positions
+ * (drafts that were rejected; 0: the request has ended) and gets n_new[b] new ones:
+ *   1. kept = min(max(keep[b], 0), kv_len[b]); the pages behind ceil(kept / page) are given back: their refs count one
+ *      less, their table entries become -1
+ *   2. a sequence with n = max(n_new[b], 0) > 0 is refused (status) if n > n_max or kept + n > l_max; else if kept is no
+ *      multiple of page and the refs of the page of position kept are more than 1; else if the new pages that it
+ *      and the sequences before it ask for are more than are free and it asks for any; else if its new rows and those of
+ *      the sequences before it are more than T.  (One that is refused by the first two rules asks for nothing.)
+ *      A refused sequence keeps its `kept` positions and gets no new one
+ *   3. the j-th new page, counted through the sequences and their positions, is the j-th free page of the pool; its
+ *      refs become 1
+ *   4. kv_len = kept + n, start = the running sum of the n; seq, pos, slot of the T rows
+ * Everything is decided on the device: a captured call follows keep and n_new, and what the tables hold.  Called again with the
+ * same keep (none above kv_len) and n_new it gives the same tables.
+ *   keep       device int32 [B], or NULL: everything is kept
+ *   n_new      device int32 [B]
+ *   workspace  device, >= lrqk_pages_advance_workspace_bytes(shape), 256-byte aligned
+ * Table entries that are no pages are left out of the counting.  B, T, n_max, l_max, page, n_pages and max_pages of
+ * the shape are used.
+ */
+int lrqk_pages_advance(const lrqk_pages_shape* shape, const lrqk_pages_tables* tables, const int32_t* keep,
+                       const int32_t* n_new, void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Instrumentation (not part of the method): GPU time of the kernels of lrqk_decode_step, each
  * taken from a pair of HIP events attached to the kernel itself (they hold its own start and
  * end, so neither the gaps between launches nor the events' own cost are included).

@@ -16,6 +16,10 @@ from .binding import (  # noqa: F401
     LRQK_PAGE_BF16, LRQK_PAGE_E2M1, LRQK_PAGE_E4M3, LRQK_PAGE_F32, LRQK_PAGE_I8, Pages, PagesShape, make_pages,
     lrqk_chunk_attend, lrqk_pages_append, lrqk_pages_read, lrqk_pages_workspace_bytes,
     lrqk_validate_pages,
+    LRQK_ROPE_BANDS, LRQK_ROPE_BASE, LRQK_ROPE_HALVES, LRQK_ROPE_LINEAR, LRQK_ROPE_PAIRS, LRQK_ROPE_PLAIN, LRQK_ROPE_RAMP,
+    Rope, lrqk_pages_rotate_append, lrqk_rope_turns, lrqk_rotate, make_rope,
+    LRQK_ADVANCE_LONG, LRQK_ADVANCE_OK, LRQK_ADVANCE_PAGES, LRQK_ADVANCE_ROWS, LRQK_ADVANCE_SHARED, PagesTables,
+    lrqk_pages_advance, lrqk_pages_advance_workspace_bytes, lrqk_pages_tables_init, make_pages_tables,
     lrqk_status_string, lrqk_validate_shape, lrqk_version, lrqk_workspace_bytes, make_layer,
 )
 from .state import LayerBuffers  # noqa: F401

@@ -16,6 +16,9 @@ LRQK_FETCH_STAGED, LRQK_FETCH_DIRECT, LRQK_FETCH_GROUP = 0, 1, 2
 LRQK_SELECT_FRESH = 0x100
 LRQK_WS_SELECT, LRQK_WS_ATTEND, LRQK_WS_UPDATE, LRQK_WS_PREFILL = 1, 2, 3, 4
 LRQK_PAGE_BF16, LRQK_PAGE_F32, LRQK_PAGE_E4M3, LRQK_PAGE_I8, LRQK_PAGE_E2M1 = 0, 1, 2, 3, 8
+LRQK_ROPE_HALVES, LRQK_ROPE_PAIRS = 0, 1
+LRQK_ROPE_PLAIN, LRQK_ROPE_LINEAR, LRQK_ROPE_BASE, LRQK_ROPE_BANDS, LRQK_ROPE_RAMP = 0, 1, 2, 3, 4
+LRQK_ADVANCE_OK, LRQK_ADVANCE_LONG, LRQK_ADVANCE_SHARED, LRQK_ADVANCE_PAGES, LRQK_ADVANCE_ROWS = 0, 1, 2, 3, 4
 
 
 class LrqkError(RuntimeError):
@@ -74,6 +77,30 @@ class Pages(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("K", "V", "K_scale", "V_scale", "table", "start", "kv_len")]
 
 
+class PagesTables(C.Structure):
+    """lrqk_pages_tables: raw pointers of the tables on the device (make_pages_tables keeps its tensors alive with it)."""
+    _fields_ = [(n, C.c_void_p) for n in ("refs", "table", "kv_len", "start", "status", "seq", "pos", "slot")]
+
+
+class Rope(C.Structure):
+    """lrqk_rope (make_rope keeps the table of turns alive with it)."""
+    _fields_ = [("layout", C.c_int32), ("rot", C.c_int32), ("back", C.c_int32), ("amplitude", C.c_float),
+                ("turns", C.c_void_p)]
+
+
+class RotateShape(C.Structure):
+    """lrqk_rotate_shape."""
+    _fields_ = [(n, C.c_int32) for n in ("T", "Hq", "Hkv", "d", "q_type", "q_out_type", "k_type", "q_stride",
+                                         "q_out_stride", "k_stride", "k_out_stride")]
+
+
+class NewRows(C.Structure):
+    """lrqk_new_rows."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int32),
+                ("k_stride", C.c_int32), ("v_stride", C.c_int32), ("q_out", C.c_void_p), ("pos", C.c_void_p),
+                ("slot", C.c_void_p)]
+
+
 class _StepDebug(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("sel_idx", "sel_slot", "hit", "miss_tok", "miss_slot",
                                           "n_miss", "link_rows")]
@@ -119,6 +146,12 @@ def load_library():
         "lrqk_pages_append": (C.c_int, [psp, pgp, vp, vp, vp]),
         "lrqk_pages_read": (C.c_int, [psp, pgp, i32, vp, vp, vp]),
         "lrqk_chunk_attend": (C.c_int, [psp, pgp, vp, vp, vp, sz, vp]),
+        "lrqk_rope_turns": (C.c_int, [i32, i32, C.c_double, C.c_double, C.c_double, C.c_double, i32, vp, C.POINTER(C.c_float)]),
+        "lrqk_rotate": (C.c_int, [C.POINTER(RotateShape), C.POINTER(Rope), vp, vp, vp, vp, vp, vp]),
+        "lrqk_pages_rotate_append": (C.c_int, [psp, pgp, C.POINTER(Rope), C.POINTER(NewRows), vp]),
+        "lrqk_pages_tables_init": (C.c_int, [psp, C.POINTER(PagesTables), vp]),
+        "lrqk_pages_advance_workspace_bytes": (sz, [psp]),
+        "lrqk_pages_advance": (C.c_int, [psp, C.POINTER(PagesTables), vp, vp, vp, sz, vp]),
         "lrqk_plan_create": (C.c_int, [sp, C.POINTER(vp)]),
         "lrqk_plan_destroy": (C.c_int, [vp]),
         "lrqk_fetch_misses": (C.c_int, [vp, sp, vp, vp, vp, vp, vp, vp, vp, C.c_int,
@@ -145,7 +178,8 @@ EXPORTS = ["lrqk_version", "lrqk_status_string", "lrqk_last_hip_error", "lrqk_va
            "lrqk_plan_time_proxy_pass", "lrqk_factor_update", "lrqk_append_token",
            "lrqk_prefill_factorize", "lrqk_sparse_attend_noalloc", "lrqk_select_state_init",
            "lrqk_validate_pages", "lrqk_pages_workspace_bytes", "lrqk_pages_append",
-           "lrqk_pages_read", "lrqk_chunk_attend"]
+           "lrqk_pages_read", "lrqk_chunk_attend", "lrqk_rope_turns", "lrqk_rotate", "lrqk_pages_rotate_append",
+           "lrqk_pages_tables_init", "lrqk_pages_advance_workspace_bytes", "lrqk_pages_advance"]
 
 
 def _check(status: int, where: str):
@@ -478,3 +512,157 @@ def lrqk_chunk_attend(shape, pages, q, out, workspace, stream=None):
         C.byref(shape), C.byref(pages), _fits(q, shape, rows), _fits(out, shape, rows),
         _dev(workspace), workspace.numel() * workspace.element_size(), _raw_stream(stream, pages, q, out)),
         "lrqk_chunk_attend")
+
+
+# ---- rotary positions --------------------------------------------------------------------------------
+def lrqk_rope_turns(rot: int, scaling: int = LRQK_ROPE_PLAIN, *, base: float, factor: float = 1.0, low: float = 1.0,
+                    high: float = 4.0, l_orig: int = 8192):
+    """The table of a rope, [rot / 2] on the host (int64 that holds the bits of uint64), and its amplitude."""
+    turns = torch.empty(max(0, int(rot)) // 2, dtype=torch.int64)
+    amplitude = C.c_float(0.0)
+    _check(load_library().lrqk_rope_turns(int(rot), int(scaling), float(base), float(factor), float(low), float(high),
+                                          int(l_orig), turns.data_ptr() or None, C.byref(amplitude)), "lrqk_rope_turns")
+    return turns, amplitude.value
+
+
+def make_rope(*, turns, rot: int, layout: int = LRQK_ROPE_HALVES, amplitude: float = 1.0, back: bool = False) -> Rope:
+    """turns: as lrqk_rope_turns gives it, on the device."""
+    if turns.dtype not in (torch.int64, torch.uint64):
+        raise TypeError(f"expected int64 or uint64, got {turns.dtype}")
+    if turns.numel() < int(rot) // 2:
+        raise ValueError(f"expected {int(rot) // 2} turns, got {turns.numel()}")
+    r = Rope(int(layout), int(rot), int(bool(back)), float(amplitude), _dev(turns))
+    r.tensor = turns
+    return r
+
+
+_KV_TYPES = {torch.bfloat16: LRQK_KV_BF16, torch.float32: LRQK_KV_F32}
+
+
+def _heads(t: torch.Tensor, T: int):
+    """Pointer, heads, type and stride of rows [T,heads,128], each token's dense; tokens may lie further apart."""
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    kind = _KV_TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"rows of {t.dtype}")
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != 128:
+        raise ValueError(f"expected [{T}, heads, 128], got {tuple(t.shape)}")
+    apart, head, one = t.stride()
+    dense = t.shape[1] * 128
+    if one != 1 or (head != 128 and t.shape[1] > 1) or (T > 1 and not dense <= apart < 1 << 31):
+        raise ValueError(f"rows of a token are not dense, or tokens overlap: strides {t.stride()}")
+    return t.data_ptr(), t.shape[1], kind, apart if T > 1 else 0
+
+
+def _here(stream, rope: Rope, *tensors):
+    """As _raw_stream, for a call on a rope."""
+    here = torch.cuda.current_device()
+    if getattr(rope, "tensor", None) is not None and rope.tensor.get_device() != here:
+        raise ValueError(f"rope on {rope.tensor.device}, current device is {here}")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, current device is {here}")
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
+
+
+def lrqk_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, stream=None):
+    """q, q_out [T,Hq,128] and k, k_out [T,Hkv,128], tokens as far apart as their strides say; pos [T] int32."""
+    T = pos.numel()
+    s = RotateShape(T=T, d=128)
+    ptr = [None, None, None, None]
+    if q is not None and q_out is not None:
+        ptr[0], s.Hq, s.q_type, s.q_stride = _heads(q, T)
+        ptr[1], heads, s.q_out_type, s.q_out_stride = _heads(q_out, T)
+        if heads != s.Hq:
+            raise ValueError(f"q of {s.Hq} heads, q_out of {heads}")
+    if k is not None and k_out is not None:
+        ptr[2], s.Hkv, s.k_type, s.k_stride = _heads(k, T)
+        ptr[3], heads, kind, s.k_out_stride = _heads(k_out, T)
+        if heads != s.Hkv or kind != s.k_type:
+            raise ValueError(f"k {tuple(k.shape)} of {k.dtype}, k_out {tuple(k_out.shape)} of {k_out.dtype}")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("an input without its output, or an output without its input")
+    _check(load_library().lrqk_rotate(C.byref(s), C.byref(rope), _dev(pos, torch.int32), *ptr,
+                                      _here(stream, rope, pos, q, q_out, k, k_out)), "lrqk_rotate")
+
+
+def lrqk_pages_rotate_append(shape, pages, rope: Rope, q, k_new, v_new, q_out, pos=None, slot=None, stream=None):
+    """q [T,Hq,128], k_new, v_new [T,Hkv,128] of shape.kv_dtype, tokens as far apart as their strides say; q_out dense.
+    q and q_out may both be None; pos and slot [T] int32 both or neither."""
+    _hold(pages, shape)
+    n, T = NewRows(), shape.T
+    if (q is None) != (q_out is None) or (pos is None) != (slot is None):
+        raise ValueError("q without q_out or pos without slot, or the other way round")
+    kinds = []
+    if q is not None:
+        n.q, heads, kind, n.q_stride = _heads(q, T)
+        if heads != shape.Hq:
+            raise ValueError(f"q of {heads} heads, Hq = {shape.Hq}")
+        kinds.append(kind)
+        n.q_out = _fits(q_out, shape, T * shape.Hq)
+    n.k, heads, kind, n.k_stride = _heads(k_new, T)
+    n.v, heads_v, kind_v, n.v_stride = _heads(v_new, T)
+    if heads != shape.Hkv or heads_v != shape.Hkv:
+        raise ValueError(f"k of {heads} heads and v of {heads_v}, Hkv = {shape.Hkv}")
+    if any(x != shape.kv_dtype for x in kinds + [kind, kind_v]):
+        raise TypeError(f"rows of another type than kv_dtype {shape.kv_dtype}")
+    if pos is not None:
+        if pos.numel() < T or slot.numel() < T:
+            raise ValueError(f"expected {T} positions and slots, got {pos.numel()} and {slot.numel()}")
+        n.pos, n.slot = _dev(pos, torch.int32), _dev(slot, torch.int32)
+    st = _raw_stream(stream, pages, q, k_new, v_new, q_out, pos, slot)
+    if getattr(rope, "tensor", None) is not None and rope.tensor.get_device() != k_new.get_device():
+        raise ValueError(f"rope on {rope.tensor.device}, rows on {k_new.device}")
+    _check(load_library().lrqk_pages_rotate_append(C.byref(shape), C.byref(pages), C.byref(rope), C.byref(n), st),
+           "lrqk_pages_rotate_append")
+
+
+# ---- tables on the device ------------------------------------------------------------------------------
+def make_pages_tables(*, refs, table, kv_len, start, status, seq=None, pos=None, slot=None) -> PagesTables:
+    """int32 tensors of one device: refs [n_pages], table [B,max_pages], kv_len and status [B], start [B+1], seq, pos, slot [T].
+    table, start and kv_len are those that make_pages takes, too."""
+    t = PagesTables(*[_dev(x, torch.int32) for x in (refs, table, kv_len, start, status, seq, pos, slot)])
+    t.tensors = dict(refs=refs, table=table, kv_len=kv_len, start=start, status=status, seq=seq, pos=pos, slot=slot)
+    t.device = refs.device.index
+    if any(x is not None and x.device.index != t.device for x in t.tensors.values()):
+        raise ValueError("tables on several devices")
+    return t
+
+
+def _tables_hold(tables: PagesTables, shape: PagesShape):
+    """The tensors of make_pages_tables have at least the sizes that `shape` says."""
+    x = getattr(tables, "tensors", None)
+    if x is None or getattr(tables, "fits", None) == bytes(shape):
+        return
+    if lrqk_validate_pages(shape) != 0:
+        return                               # the call says so
+    for name, n in (("refs", shape.n_pages), ("table", shape.B * shape.max_pages), ("kv_len", shape.B), ("start", shape.B + 1),
+                    ("status", shape.B), ("seq", shape.T), ("pos", shape.T), ("slot", shape.T)):
+        if x[name] is not None and x[name].numel() < n:
+            raise ValueError(f"{name}: expected {n} elements, got {tuple(x[name].shape)}")
+    if shape.B > 1 and x["table"].dim() == 2 and x["table"].shape[1] != shape.max_pages:
+        raise ValueError(f"table rows of {x['table'].shape[1]} entries, max_pages {shape.max_pages}")
+    tables.fits = bytes(shape)
+
+
+def lrqk_pages_tables_init(shape, tables: PagesTables, stream=None):
+    _tables_hold(tables, shape)
+    _check(load_library().lrqk_pages_tables_init(C.byref(shape), C.byref(tables), _raw_stream(stream, tables)),
+           "lrqk_pages_tables_init")
+
+
+def lrqk_pages_advance_workspace_bytes(shape) -> int:
+    return load_library().lrqk_pages_advance_workspace_bytes(C.byref(shape))
+
+
+def lrqk_pages_advance(shape, tables: PagesTables, keep, n_new, workspace, stream=None):
+    """keep [B] int32 or None (everything is kept), n_new [B] int32."""
+    _tables_hold(tables, shape)
+    for t in (keep, n_new):
+        if t is not None and t.numel() < shape.B:
+            raise ValueError(f"expected {shape.B} numbers, got {tuple(t.shape)}")
+    _check(load_library().lrqk_pages_advance(
+        C.byref(shape), C.byref(tables), _dev(keep, torch.int32), _dev(n_new, torch.int32), _dev(workspace),
+        workspace.numel() * workspace.element_size(), _raw_stream(stream, tables, keep, n_new, workspace)),
+        "lrqk_pages_advance")

@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "liblrqk.so")
 SOURCES = ["api.hip", "proxy_scores.hip", "select_topk.hip", "cache_resolve.hip", "select_resolve.hip",
            "select_packed.hip", "select_scores.hip",
            "sparse_attend.hip", "fetch.hip", "factor_update.hip", "factor_update_small.hip",
-           "append_token.hip", "prefill.hip", "pages.hip", "chunk_attend.hip",
+           "append_token.hip", "prefill.hip", "pages.hip", "chunk_attend.hip", "rotary.hip", "page_tables.hip",
            "instrument.hip", "noalloc.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -174,6 +174,47 @@ __device__ __forceinline__ Codes8<PAGE> encode8(const float (&x)[8], uint32_t by
   }
 }
 
+// Eight elements of a row, chunk c of 16, as they are, and as fp32.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* base, int64_t row, int c, uint4& a, uint4& b) {
+  const uint4* p = static_cast<const uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
+  a = p[0];
+  if (!BF16) b = p[1];
+}
+template <bool BF16>
+__device__ __forceinline__ void store8(void* base, int64_t row, int c, uint4 a, uint4 b) {
+  uint4* p = static_cast<uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
+  p[0] = a;
+  if (!BF16) p[1] = b;
+}
+template <bool BF16>
+__device__ __forceinline__ void get8(uint4 a, uint4 b, float (&x)[8]) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    x[i] = __uint_as_float(!BF16 ? w[i] : i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xffff0000u);
+}
+
+// Those of a pool's row as the pages hold them; 16 lanes take part.  A row of codes has its four blocks of 32 elements in four
+// lanes each: a block's largest magnitude takes two DPP steps.
+template <bool BF16, int PAGE>
+__device__ __forceinline__ void put_row(void* pool, uint8_t* scale, int64_t row, int c, uint4 a, uint4 b) {
+  if constexpr (!coded(PAGE)) {
+    store8<BF16>(pool, row, c, a, b);
+  } else {
+    float x[8];
+    get8<BF16>(a, b, x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, dev::dpp_u32<0xB1>(top));  // over the four lanes of a block
+    top = max(top, dev::dpp_u32<0x4E>(top));
+    const uint32_t byte = scale_byte<PAGE>(top);
+    static_cast<Codes8<PAGE>*>(pool)[row * 16 + c] = encode8<PAGE>(x, byte);
+    if ((c & 3) == 0) scale[row * kScales + (c >> 2)] = (uint8_t)byte;
+  }
+}
+
 // Sequence that each packed row t belongs to, or -1; the whole wavefront asks, each lane for its own rows: the starts are
 // read once, 64 at a time, without a chain of dependent loads.
 template <int N>

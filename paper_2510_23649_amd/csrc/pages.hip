@@ -47,27 +47,6 @@ constexpr int kMoveThreads = 256;
 constexpr int kAppendEach = 4;                                   // rows of K and of V a 16-lane group has in flight
 constexpr int kAppendRows = kMoveThreads / 16 * kAppendEach;     // rows of K (and of V) a workgroup
 
-// Eight elements of a row, chunk c of 16, as they are, and as fp32.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t row, int c, uint4& a, uint4& b) {
-  const uint4* p = static_cast<const uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
-  a = p[0];
-  if (!BF16) b = p[1];
-}
-template <bool BF16>
-__device__ __forceinline__ void store8(void* base, int64_t row, int c, uint4 a, uint4 b) {
-  uint4* p = static_cast<uint4*>(base) + (row * 16 + c) * (BF16 ? 1 : 2);
-  p[0] = a;
-  if (!BF16) p[1] = b;
-}
-template <bool BF16>
-__device__ __forceinline__ void get8(uint4 a, uint4 b, float (&x)[8]) {
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    x[i] = __uint_as_float(!BF16 ? w[i] : i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xffff0000u);
-}
-
 // A 16-lane group takes rows of k_new and v_new, 8 elements a lane; the rows are on their way while their places are found.
 // A row of codes has its four blocks of 32 elements in four lanes each: a block's largest magnitude takes two DPP steps.
 // Bound by memory: 4 prompts of up to 8192 tokens, bf16 to e4m3 (K and V, 99 MB), 22 us.  One
@@ -99,24 +78,8 @@ __global__ __launch_bounds__(kMoveThreads) void pages_append_kernel(const Map m,
       if (t[j] < q.first || t[j] >= q.first + q.n || p < 0 || p >= m.l_max) continue;
       const int64_t row = row_of(m, b[j], (int)((uint32_t)r % (uint32_t)m.Hkv), p);
       if (row < 0) continue;
-      if constexpr (!coded(PAGE)) {
-        store8<BF16>(K, row, c, k[j], k2[j]);
-        store8<BF16>(V, row, c, v[j], v2[j]);
-      } else {
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-          float x[8];
-          get8<BF16>(which ? v[j] : k[j], which ? v2[j] : k2[j], x);
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-          top = max(top, dev::dpp_u32<0xB1>(top));  // over the four lanes of a block
-          top = max(top, dev::dpp_u32<0x4E>(top));
-          const uint32_t byte = scale_byte<PAGE>(top);
-          static_cast<Codes8<PAGE>*>(which ? V : K)[row * 16 + c] = encode8<PAGE>(x, byte);
-          if ((c & 3) == 0) (which ? V_scale : K_scale)[row * kScales + (c >> 2)] = (uint8_t)byte;
-        }
-      }
+      put_row<BF16, PAGE>(K, K_scale, row, c, k[j], k2[j]);
+      put_row<BF16, PAGE>(V, V_scale, row, c, v[j], v2[j]);
     }
   }
 }
