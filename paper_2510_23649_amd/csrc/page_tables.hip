@@ -1,8 +1,8 @@
 // g5 -- block tables and slot maps of the paged cache, made on the device (include/lrqk.h).
 //
 // A few kilobytes that depend on each other: bound by latency.  One workgroup does all of it for one call, with barriers in
-// place of launches; the maps of many rows are a second launch.  Which page a sequence gets depends on nothing but the set of
-// free pages, so the order in which atomics give pages back does not show.
+// place of launches; the maps of many rows are a launch more, the counts of a large pool two.  Which page a sequence gets depends on
+// nothing but the set of free pages, so the order in which atomics give pages back does not show.
 #include "pages.h"
 
 #include <algorithm>
@@ -14,36 +14,48 @@ using namespace pages;
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSeqs = 2048;        // sequences whose numbers LDS holds
-constexpr int kTile = kThreads * 16;  // pages looked at a time: a wavefront takes 1024 of them, four loads of four a lane
-constexpr int kRowsHere = 8192;    // rows whose maps the one workgroup makes
+constexpr int kSeqs = 2048;           // sequences whose numbers LDS holds
+constexpr int kTile = kThreads * 16;  // pages looked at together: a wavefront takes 1024 of them, four loads of four a lane
+constexpr int kRowsHere = 4096;       // rows whose maps the one workgroup makes; with more a second launch is shorter
+// Pages whose counts the one workgroup looks through: 64K of them take it 4.5 us, and two launches 5 however many there are.
+constexpr int kPagesHere = 4 * kTile;
 
 struct Args {
   int32_t *refs, *table, *kv_len, *start, *status, *seq, *pos, *slot;
   const int32_t *keep, *n_new;
-  int32_t* work;  // B > kSeqs: what LDS does not hold
+  int32_t* work;    // B > kSeqs: what LDS does not hold
+  int32_t* counts;  // n_pages > kPagesHere: free pages of each tile, after what is given back; else null
   int B, T, n_max, l_max, n_pages, max_pages, page_log2;
   bool maps;      // of the rows, here
 };
 
 __device__ __forceinline__ int pages_of(const Args& a, int len) { return (len + (1 << a.page_log2) - 1) >> a.page_log2; }
 
-// Sum over the workgroup's threads before this one, and of all: a wavefront's sum of numbers below 2^24 fits 32 bits, the
-// workgroup's need not.
-__device__ __forceinline__ uint64_t scan(uint32_t v, uint32_t* tot, uint64_t& all) {
+// Sums over the workgroup's threads before this one, and of all, of two numbers at a time: a wavefront's sum of numbers up to 2^24
+// fits 32 bits, the workgroup's need not.  One barrier: the totals of one scan are read while the next one writes the others.
+struct Totals {
+  uint2 of[2][kWaves];
+};
+struct Sums {
+  uint64_t x, y, all_x, all_y;
+};
+__device__ __forceinline__ Sums scan(uint32_t x, uint32_t y, Totals& tot, int& turn) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const uint32_t upto = dev::wave_inclusive_scan(v);
-  __syncthreads();  // (tot may still be read)
-  if (lane == 63) tot[w] = upto;
+  const uint32_t ux = dev::wave_inclusive_scan(x), uy = dev::wave_inclusive_scan(y);
+  uint2* const of = tot.of[turn];
+  turn ^= 1;
+  if (lane == 63) of[w] = make_uint2(ux, uy);
   __syncthreads();
-  uint64_t before = 0;
-  all = 0;
+  Sums s{ux - x, uy - y, 0, 0};
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    before += i < w ? tot[i] : 0u;
-    all += tot[i];
+    const uint2 t = of[i];
+    s.x += i < w ? t.x : 0u;
+    s.y += i < w ? t.y : 0u;
+    s.all_x += t.x;
+    s.all_y += t.y;
   }
-  return before + upto - v;
+  return s;
 }
 
 // The last of x[0 .. n) (ascending, x[0] <= v) that is not above v.
@@ -61,18 +73,34 @@ __device__ __forceinline__ int last_upto(const int32_t* x, int n, int v) {
 __device__ __forceinline__ uint32_t free_mask(const Args& a, int64_t base, int w, int lane) {
   uint32_t mask = 0;
   const int64_t first = base + w * 1024 + 4 * lane;
+  int4 r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t p = first + 256 * i;
     if (p + 4 <= a.n_pages) {
-      const int4 r = *reinterpret_cast<const int4*>(a.refs + p);
-      mask |= ((r.x <= 0 ? 1u : 0u) | (r.y <= 0 ? 2u : 0u) | (r.z <= 0 ? 4u : 0u) | (r.w <= 0 ? 8u : 0u)) << (4 * i);
+      r[i] = *reinterpret_cast<const int4*>(a.refs + p);
     } else {
-      for (int j = 0; j < 4; ++j)
-        if (p + j < a.n_pages && a.refs[p + j] <= 0) mask |= 1u << (4 * i + j);
+      r[i].x = p < a.n_pages ? a.refs[p] : 1;
+      r[i].y = p + 1 < a.n_pages ? a.refs[p + 1] : 1;
+      r[i].z = p + 2 < a.n_pages ? a.refs[p + 2] : 1;
+      r[i].w = 1;
     }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    mask |= ((r[i].x <= 0 ? 1u : 0u) | (r[i].y <= 0 ? 2u : 0u) | (r[i].z <= 0 ? 4u : 0u) | (r[i].w <= 0 ? 8u : 0u)) << (4 * i);
   return mask;
+}
+// Free pages of the wavefront in front of each of the lane's four groups of four; returns those of the wavefront.
+__device__ __forceinline__ uint32_t in_wave(uint32_t mask, uint32_t (&before)[4]) {
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t k = (uint32_t)__builtin_popcount(mask >> (4 * i) & 15u), upto = dev::wave_inclusive_scan(k);
+    before[i] = n + upto - k;
+    n += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return n;
 }
 
 __device__ __forceinline__ void put_maps(const Args& a, int t, int b, int pos, int page) {
@@ -81,84 +109,154 @@ __device__ __forceinline__ void put_maps(const Args& a, int t, int b, int pos, i
   if (a.slot) a.slot[t] = (unsigned)page >= (unsigned)a.n_pages ? -1 : (page << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
 }
 
-__global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
-  __shared__ int32_t lds[4 * (kSeqs + 1)];
-  __shared__ uint32_t tot[kWaves];
-  __shared__ int32_t most;
-  int32_t* const own = a.B <= kSeqs ? lds : a.work;
-  int32_t* const kept = own;                // [B] positions kept
-  int32_t* const want = kept + (a.B + 1);   // [B] new tokens, or -status
-  int32_t* const rank = want + (a.B + 1);   // [B] new pages of the sequences before
-  int32_t* const start = rank + (a.B + 1);  // [B+1]
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// Positions kept of b's `old`.
+__device__ __forceinline__ int kept_of(const Args& a, int b, int& old) {
+  old = min(max(a.kv_len[b], 0), a.l_max);
+  return a.keep ? min(max(a.keep[b], 0), old) : old;
+}
 
-  // 1: cut back
+// Step 1 by a wavefront a sequence, and the tiles' counts, of a large pool.
+__global__ __launch_bounds__(256) void cut_kernel(const Args a) {
+  const int lane = threadIdx.x & 63, b = (int)(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (b >= a.B) return;
+  int old;
+  const int k = kept_of(a, b, old), to = pages_of(a, old);
+  int32_t* const row = a.table + (size_t)b * a.max_pages;
+  for (int i = pages_of(a, k) + lane; i < to; i += 64) {
+    const int pg = row[i];
+    row[i] = -1;
+    if ((unsigned)pg < (unsigned)a.n_pages) atomicSub(a.refs + pg, 1);
+  }
+}
+__global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
+  __shared__ Totals tot;
+  int turn = 0;
+  const uint32_t mask = free_mask(a, (int64_t)blockIdx.x * kTile, threadIdx.x >> 6, threadIdx.x & 63);
+  const Sums s = scan((uint32_t)__builtin_popcount(mask), 0u, tot, turn);
+  if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)s.all_x;
+}
+
+template <bool LDS>
+__global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
+  __shared__ int32_t lds[LDS ? 4 * (kSeqs + 1) : 1];
+  __shared__ uint16_t pick[kTile];  // free pages of a tile, ascending
+  __shared__ Totals tot;
+  __shared__ int32_t most, first_tile;
+  const int size = LDS ? kSeqs + 1 : a.B + 1;
+  int32_t* const kept = LDS ? lds : a.work;  // [B] positions kept
+  int32_t* const want = kept + size;         // [B] new tokens, or -status
+  int32_t* const rank = want + size;         // [B] table entries given back, then new pages, of the sequences before
+  int32_t* const start = rank + size;        // [B+1]
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, page = 1 << a.page_log2;
+  int turn = 0;
+
+  // 1: cut back.  Each thread takes entries that are given back wherever they are: a loop over a sequence's would wait for
+  // one load after the other (28 us instead of 10 for 256 sequences, of which a third give something back).
+  uint64_t gone = 0;
+  int last = -1;  // the page of position `kept`, if that is no page's first (one sequence a thread: looked up on the way)
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
-    int held = 0, keep_pages = 0;
+    int n_gone = 0;
     if (b < a.B) {
-      const int old = min(max(a.kv_len[b], 0), a.l_max), n = max(a.n_new[b], 0);
-      const int k = a.keep ? min(max(a.keep[b], 0), old) : old;
-      held = pages_of(a, old);
-      keep_pages = pages_of(a, k);
+      const int n = max(a.n_new[b], 0);
+      int old;
+      const int k = kept_of(a, b, old);
+      n_gone = a.counts ? 0 : pages_of(a, old) - pages_of(a, k);
       kept[b] = k;
       want[b] = n > 0 && (n > a.n_max || n > a.l_max - k) ? -LRQK_ADVANCE_LONG : n;
+      if ((k & (page - 1)) != 0) last = a.table[(size_t)b * a.max_pages + (k >> a.page_log2)];
     }
-    uint64_t todo = __ballot(held > keep_pages);
-    while (todo) {
-      const int j = __builtin_ctzll(todo);
-      todo &= todo - 1;
-      const int to = __builtin_amdgcn_readlane(held, j);
-      int32_t* row = a.table + (size_t)(b0 + w * 64 + j) * a.max_pages;
-      for (int i = __builtin_amdgcn_readlane(keep_pages, j) + lane; i < to; i += 64) {
-        const int pg = row[i];
-        row[i] = -1;
-        if ((unsigned)pg < (unsigned)a.n_pages) atomicSub(a.refs + pg, 1);
-      }
-    }
+    const Sums s = scan((uint32_t)n_gone, 0u, tot, turn);
+    if (b < a.B) rank[b] = (int32_t)min(gone + s.x, (uint64_t)INT32_MAX);
+    gone += s.all_x;
   }
-  if (threadIdx.x == 0) most = 0;
+  if (threadIdx.x == 0) {
+    most = 0;
+    first_tile = INT32_MAX;
+  }
+  __syncthreads();
+  for (uint64_t i = threadIdx.x; i < gone; i += kThreads) {
+    if (i >= INT32_MAX) break;  // (2^31 entries: no table has them)
+    const int b = last_upto(rank, a.B, (int)i);
+    int32_t* const entry = a.table + (size_t)b * a.max_pages + pages_of(a, kept[b]) + ((int)i - rank[b]);
+    const int pg = *entry;
+    *entry = -1;
+    if ((unsigned)pg < (unsigned)a.n_pages) atomicSub(a.refs + pg, 1);
+  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the atomics have arrived in the L2, past which nothing has read refs
   __syncthreads();
 
   // 2: what is asked for
-  uint64_t pages = 0, rows = 0;  // of the sequences so far
+  uint64_t asked = 0, rows = 0;
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
     int n = 0, need = 0;
     if (b < a.B) {
       n = want[b];
-      const int k = kept[b], kp = pages_of(a, k);
-      if (n > 0 && (k & ((1 << a.page_log2) - 1)) != 0) {
-        const int pg = a.table[(size_t)b * a.max_pages + kp - 1];
+      const int k = kept[b];
+      if (n > 0 && (k & (page - 1)) != 0) {
+        const int pg = a.B <= kThreads ? last : a.table[(size_t)b * a.max_pages + (k >> a.page_log2)];
         if ((unsigned)pg < (unsigned)a.n_pages && a.refs[pg] > 1) want[b] = n = -LRQK_ADVANCE_SHARED;
       }
-      need = n > 0 ? pages_of(a, k + n) - kp : 0;
+      need = n > 0 ? pages_of(a, k + n) - pages_of(a, k) : 0;
       n = max(n, 0);
     }
-    uint64_t all;
-    const uint64_t p = pages + scan((uint32_t)need, tot, all);
-    pages += all;
-    const uint64_t r = rows + scan((uint32_t)n, tot, all);
-    rows += all;
+    const Sums s = scan((uint32_t)need, (uint32_t)n, tot, turn);
     if (b < a.B) {
-      rank[b] = (int32_t)min(p, (uint64_t)INT32_MAX);
-      if (n > 0 && r + n > (uint64_t)a.T) start[b] = LRQK_ADVANCE_ROWS;
-      else start[b] = 0;
+      rank[b] = (int32_t)min(asked + s.x, (uint64_t)INT32_MAX);
+      start[b] = n > 0 && rows + s.y + n > (uint64_t)a.T ? LRQK_ADVANCE_ROWS : 0;
     }
+    asked += s.all_x;
+    rows += s.all_y;
   }
-  const uint64_t asked = pages;
 
   // free pages: as many as are asked for, or all
   uint64_t there = 0;
-  int64_t from = 0;  // the first tile that has any
-  for (int64_t base = 0; base < a.n_pages && there < asked; base += kTile) {
-    uint64_t all;
-    scan((uint32_t)__builtin_popcount(free_mask(a, base, w, lane)), tot, all);
-    if (there == 0) from = base;
-    there += all;
+  int64_t from = 0, at = -1;  // the first tile that has any; the one that `mask` is of
+  uint32_t mask = 0, before[4];
+  uint64_t ahead = 0, in_tile = 0;
+  auto count = [&]() __attribute__((always_inline)) {  // what `mask` says
+    const uint32_t n = in_wave(mask, before);
+    const Sums s = scan(lane == 0 ? n : 0u, 0u, tot, turn);
+    ahead = __builtin_amdgcn_readfirstlane((uint32_t)s.x);  // of lane 0: the wavefronts before
+    in_tile = s.all_x;
+  };
+  if (a.counts && asked > 0) {
+    const int tiles = (int)((a.n_pages + (int64_t)kTile - 1) / kTile);
+    for (int i0 = 0; i0 < tiles && there < asked; i0 += kThreads) {
+      const int n = i0 + (int)threadIdx.x < tiles ? a.counts[i0 + threadIdx.x] : 0;
+      if (n > 0) atomicMin(&first_tile, i0 + (int)threadIdx.x);
+      there += scan((uint32_t)n, 0u, tot, turn).all_x;
+    }
+    from = first_tile == INT32_MAX ? 0 : (int64_t)first_tile * kTile;
+  } else if (asked > 0) {
+    mask = free_mask(a, 0, w, lane);
+    count();
+    there = in_tile;
+    at = 0;
+    // four tiles a round (64K pages: 2 us, and 1.5 a tile where they come one by one); a wavefront's 1024 of each fit 16 bits
+    for (int64_t base = kTile; base < a.n_pages && there < asked; base += 4 * kTile) {
+      uint32_t n[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n[i] = (uint32_t)__builtin_popcount(free_mask(a, base + i * kTile, w, lane));
+      const Sums s = scan(n[0] | n[1] << 16, n[2] | n[3] << 16, tot, turn);
+      (void)s;
+      uint32_t in[4] = {0, 0, 0, 0};
+      const uint2* const of = tot.of[turn ^ 1];
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        in[0] += of[i].x & 0xffffu;
+        in[1] += of[i].x >> 16;
+        in[2] += of[i].y & 0xffffu;
+        in[3] += of[i].y >> 16;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (there == 0) from = base + i * kTile;
+        there += in[i];
+      }
+    }
   }
-  __syncthreads();
 
   // 2, 4: who gets what
   rows = 0;
@@ -178,13 +276,12 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
       // those that are refused pages or rows are the last ones that ask for any: the others' pages are the first ones
       if (n > 0 && need > 0) atomicMax(&most, rank[b] + need);
     }
-    uint64_t all;
-    const uint64_t r = rows + scan((uint32_t)n, tot, all);
-    rows += all;
+    const Sums s = scan((uint32_t)n, 0u, tot, turn);
     if (b < a.B) {
-      start[b] = (int32_t)r;
-      a.start[b] = (int32_t)r;
+      start[b] = (int32_t)(rows + s.x);
+      a.start[b] = (int32_t)(rows + s.x);
     }
+    rows += s.all_x;
   }
   if (threadIdx.x == 0) {
     start[a.B] = (int32_t)rows;
@@ -192,49 +289,51 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   }
   __syncthreads();
 
-  // 3: the pages
+  // 3: the pages: a tile's free ones in order, then a thread for each that is given away
   const int give = most;
   int64_t found = 0;
   for (int64_t base = from; base < a.n_pages && found < give; base += kTile) {
-    const uint32_t mask = free_mask(a, base, w, lane);
-    uint32_t before[4], in_wave = 0;
+    if (a.counts && a.counts[base / kTile] == 0) continue;
+    if (base != at) {
+      mask = free_mask(a, base, w, lane);
+      count();
+    }
+    at = -1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t n = (uint32_t)__builtin_popcount(mask >> (4 * i) & 15u), upto = dev::wave_inclusive_scan(n);
-      before[i] = in_wave + upto - n;
-      in_wave += __builtin_amdgcn_readlane(upto, 63);
-    }
-    uint64_t all;
-    uint64_t ahead = scan(lane == 0 ? in_wave : 0u, tot, all);  // of lane 0: the wavefronts before
-    ahead = __builtin_amdgcn_readfirstlane((uint32_t)ahead);
+      uint32_t r = (uint32_t)ahead + before[i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int64_t r = found + (int64_t)ahead + before[i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!(mask >> (4 * i + j) & 1)) continue;
-        if (r < give) {
-          const int page = (int)(base + w * 1024 + 256 * i + 4 * lane + j);
-          const int b = last_upto(rank, a.B, (int)r);
-          a.refs[page] = 1;
-          a.table[(size_t)b * a.max_pages + pages_of(a, kept[b]) + ((int)r - rank[b])] = page;
-        }
-        ++r;
-      }
+      for (int j = 0; j < 4; ++j)
+        if (mask >> (4 * i + j) & 1) pick[r++] = (uint16_t)(w * 1024 + 256 * i + 4 * lane + j);
     }
-    found += (int64_t)all;
+    __syncthreads();
+    const int n = (int)min((int64_t)in_tile, give - found);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const int r = (int)found + i, pg = (int)base + pick[i];
+      const int b = last_upto(rank, a.B, r);
+      a.refs[pg] = 1;
+      a.table[(size_t)b * a.max_pages + pages_of(a, kept[b]) + (r - rank[b])] = pg;
+    }
+    found += (int64_t)in_tile;
+    __syncthreads();
   }
   if (!a.maps) return;
-  __syncthreads();
   const int n_rows = start[a.B];
-  for (int t = threadIdx.x; t < a.T; t += kThreads) {
-    if (t >= n_rows) {
-      put_maps(a, t, -1, -1, -1);
-      continue;
+  for (int t0 = threadIdx.x; t0 < a.T; t0 += 4 * kThreads) {
+    int b[4], pos[4], pg[4];  // together, not one after the other
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + i * kThreads;
+      b[i] = pos[i] = pg[i] = -1;
+      if (t < n_rows) {
+        b[i] = last_upto(start, a.B, t);
+        pos[i] = kept[b[i]] + (t - start[b[i]]);
+        if (a.slot) pg[i] = a.table[(size_t)b[i] * a.max_pages + (pos[i] >> a.page_log2)];
+      }
     }
-    const int b = last_upto(start, a.B, t);
-    const int pos = kept[b] + (t - start[b]);
-    put_maps(a, t, b, pos, a.slot ? a.table[(size_t)b * a.max_pages + (pos >> a.page_log2)] : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t0 + i * kThreads < a.T) put_maps(a, t0 + i * kThreads, b[i], pos[i], pg[i]);
   }
 }
 
@@ -255,7 +354,7 @@ __global__ __launch_bounds__(kMapThreads) void maps_kernel(const Args a) {
       continue;
     }
     const int b = last_upto(start, a.B, t);
-    const int pos = a.kv_len[b] - start[b + 1] + t;
+    const int pos = a.kv_len[b] - start[b + 1] + t;  // kv_len - n + (t - start[b])
     put_maps(a, t, b, pos, a.slot ? a.table[(size_t)b * a.max_pages + (pos >> a.page_log2)] : 0);
   }
 }
@@ -267,13 +366,20 @@ __global__ __launch_bounds__(kMapThreads) void tables_init_kernel(const Args a) 
   for (int64_t i = i0; i < a.B; i += step) a.kv_len[i] = 0;
 }
 
+size_t work_bytes(const lrqk_pages_shape& s) {
+  return s.B <= kSeqs ? 0 : round_up((size_t)4 * (s.B + 1) * sizeof(int32_t), 256);
+}
+size_t count_bytes(const lrqk_pages_shape& s) {
+  return s.n_pages <= kPagesHere ? 0 : ((size_t)s.n_pages + kTile - 1) / kTile * sizeof(int32_t);
+}
+
 bool given(std::initializer_list<const void*> p) {
   for (const void* x : p)
     if (!x || !aligned16(x)) return false;
   return true;
 }
 Args make_args(const lrqk_pages_shape& s, const lrqk_pages_tables& t) {
-  return Args{t.refs, t.table, t.kv_len, t.start, t.status, t.seq, t.pos, t.slot, nullptr, nullptr, nullptr,
+  return Args{t.refs, t.table, t.kv_len, t.start, t.status, t.seq, t.pos, t.slot, nullptr, nullptr, nullptr, nullptr,
               s.B, s.T, s.n_max, s.l_max, s.n_pages, s.max_pages, __builtin_ctz((unsigned)s.page), true};
 }
 
@@ -285,7 +391,7 @@ Args make_args(const lrqk_pages_shape& s, const lrqk_pages_tables& t) {
 LRQK_API size_t lrqk_pages_advance_workspace_bytes(const lrqk_pages_shape* shape) {
   using namespace lrqk;
   if (check_pages(shape) != LRQK_OK) return 0;
-  return shape->B <= kSeqs ? 256 : round_up((size_t)4 * (shape->B + 1) * sizeof(int32_t), 256);
+  return round_up(256 + work_bytes(*shape) + count_bytes(*shape), 256);
 }
 
 LRQK_API int lrqk_pages_tables_init(const lrqk_pages_shape* shape, const lrqk_pages_tables* tables, void* stream) {
@@ -317,7 +423,13 @@ LRQK_API int lrqk_pages_advance(const lrqk_pages_shape* shape, const lrqk_pages_
   const bool any = a.seq || a.pos || a.slot;
   a.maps = any && a.T <= kRowsHere;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(advance_kernel, dim3(1), dim3(kThreads), 0, st, a);
+  if (count_bytes(*shape) > 0) {
+    a.counts = a.work + work_bytes(*shape) / sizeof(int32_t);
+    hipLaunchKernelGGL(cut_kernel, dim3((unsigned)ceil_div(a.B, 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(count_kernel, dim3((unsigned)((a.n_pages + (int64_t)kTile - 1) / kTile)), dim3(kThreads), 0, st, a);
+  }
+  if (a.B <= kSeqs) hipLaunchKernelGGL(advance_kernel<true>, dim3(1), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(advance_kernel<false>, dim3(1), dim3(kThreads), 0, st, a);
   if (any && !a.maps)
     hipLaunchKernelGGL(maps_kernel, dim3((unsigned)std::min(ceil_div(a.T, kMapThreads), 2048)), dim3(kMapThreads), 0, st, a);
   LRQK_HIP(hipGetLastError());
