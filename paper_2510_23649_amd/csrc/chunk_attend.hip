@@ -43,6 +43,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.0f;
 constexpr float kHeavy = 4096.0f;
 constexpr float kFar = 1073741824.0f;  // see Rows::weigh
+constexpr int kFewWaves = 2;           // wavefronts a SIMD of attend_few_kernel
 constexpr int kPartial = kPartialStride;  // floats of a partial state: max, sum, 2 unused, acc[128]
 
 struct Args {
@@ -1091,6 +1092,264 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   }
 }
 
+// ---- 16 rows of the problem in a wavefront, pages of 4 bits --------------------------------------------------
+// Lane l: row l % 16; the 16 positions of a tile of S^T are 4 (l / 16) + v, v the register; elements of O^T likewise.  A row of
+// K goes straight from its load into the product: the sum over elements may run in any order, so that the lane that holds
+// 32 codes of a row, one block with one scale, multiplies them eight at a time with those eight of its q.
+struct Rows16 {
+  uint4 q[4];   // elements 32 (l / 16) + 8 s .. + 7
+  f32x4 o[8];   // elements 16 t ..
+  float mx, sum;
+  int see;
+
+  __device__ __forceinline__ void start(const void* base, int64_t row, bool negate, int lane) {
+    const uint32_t flip = negate ? 0x80008000u : 0u;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      uint4 x = static_cast<const uint4*>(base)[row * 16 + 4 * (lane >> 4) + s];
+      x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+      q[s] = x;
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    mx = -INFINITY;
+    sum = 0.0f;
+  }
+  // scores of 16 positions: codes of row l % 16, block l / 16
+  __device__ __forceinline__ f32x4 scores(const uint4 codes, uint32_t byte) const {
+    const float f = scale_of(byte);
+    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, decode8_bf16<LRQK_PAGE_E2M1>(w[k], f)),
+                                                  __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
+    return s;
+  }
+  // scores of the 16 positions from p0 that the row does not see, or that are not there, become -infinity
+  __device__ __forceinline__ void mask(f32x4& s, int p0, uint32_t there, int lane) const {
+    const int up_to = see - p0;
+    const uint32_t mine = (up_to >= 16 ? there : up_to <= 0 ? 0u : there & ((1u << up_to) - 1)) >> (4 * (lane >> 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = mine & (1u << e) ? s[e] : -INFINITY;
+  }
+  static __device__ __forceinline__ float over_lanes(float x) {  // the largest of the four lanes of a row
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  }
+  static __device__ __forceinline__ float sum_lanes(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+  }
+  __device__ __forceinline__ void raise(float top) {
+    const float to = fmaxf(mx, top);
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mx - to);
+    sum *= f;
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[t][e] *= f;
+    mx = to;
+  }
+  // Weights of 64 positions (see Rows::weigh and weigh_any) as the second product's operands, 32 each, at a maximum that is
+  // raised where it has to be.
+  __device__ __forceinline__ void settle(const f32x4 (&s)[4], float c, uint4 (&x)[2]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+    top = over_lanes(top) * c;
+    if (__any(top > mx + kLag)) raise(top);
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    const auto form = [&](auto weight) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = weight(s[2 * i + e / 4][e % 4]);
+        x[i] = make_uint4(dev::pack_bf16(w[0], w[1]), dev::pack_bf16(w[2], w[3]), dev::pack_bf16(w[4], w[5]), dev::pack_bf16(w[6], w[7]));
+      }
+    };
+    form([&](float y) { return __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, -base)); });
+    if (__builtin_expect(__any(fabsf(mx) >= kFar), 0)) {
+      asm volatile("");  // a branch, which next to no call takes
+      const bool rounded = fabsf(mx) >= kFar;
+      form([&](float y) {
+#pragma clang fp contract(off)
+        const float z = y * c;
+        return __builtin_amdgcn_exp2f(rounded ? z - base : __builtin_fmaf(y, c, -base));
+      });
+    }
+    const dev::bf16x2 one = __builtin_bit_cast(dev::bf16x2, 0x3f803f80u);
+    float add = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) add = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e]), one, add, false);
+    }
+    sum += add;
+  }
+  // O += weights of 32 positions times their V rows.  The weights' order: 4 (l / 16) + j, then 16 + 4 (l / 16) + j.
+  __device__ __forceinline__ void output(const char* vt, const uint4 x, int lane) {
+    const int g = lane & 15, row = 4 * (lane >> 4) + (g >> 2);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      s16x4 v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(vt + chunk(row + 16 * j, 2 * t + ((g & 3) >> 1)) + 8 * (g & 1)));
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), __builtin_bit_cast(bf16x8, x), o[t], 0, 0, 0);
+    }
+  }
+  // Where LDS holds chunk c of a row: eight rows' same chunk (as they are stored) lies in eight places mod 8, eight rows' two
+  // chunks (as they are read) in sixteen.
+  static __device__ __forceinline__ int chunk(int row, int c) {
+    return row * kRowB<true> + ((c ^ (((row & 7) << 1) | ((row >> 2) & 1))) << 4);
+  }
+};
+
+// At most 16 rows a workgroup, pages of 4 bits: a wavefront takes every fourth block of 64 positions, four tiles of 16, each of
+// which lies in one page.  K does not touch LDS; V passes through 8 KB of it, 32 positions at a time.
+__global__ __launch_bounds__(kThreads, kFewWaves) void attend_few_kernel(const Args a) {
+  constexpr int M = 16, BN = 64, kTile = 32 * kRowB<true>;
+  __shared__ __align__(16) char lds[kWaves * kTile];
+  __shared__ float wm[kWaves * M], ws[kWaves * M];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % a.m.Hkv;
+  const uint4* const K = static_cast<const uint4*>(a.K);
+  const uint4* const V = static_cast<const uint4*>(a.V);
+  for (int unit = blockIdx.x / a.m.Hkv;; unit += gridDim.x / a.m.Hkv) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
+    Problem p;
+    if (!find_unit<M, false>(a, unit, p)) return;
+    const int rows = min(M, p.rows - p.r0);
+    const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
+    const int from = p.piece * p.step, end = min(most, from + p.step);
+    if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
+    Rows16 r;
+    const int real = min(p.r0 + (lane & 15), p.rows - 1);
+    r.see = sees(a, p, real);
+    r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    const float c = log2_scale(a);
+    char* const vt = lds + w * kTile;
+    bool cleared = false;
+    const int mine = from + w * BN;
+    if (mine < end) {
+      const int32_t* const table = a.m.table + (size_t)p.b * a.m.max_pages;
+      const uint32_t in_page = (1u << a.m.page_log2) - 1;
+      const uint32_t at = 4 * (lane & 15) + (lane >> 4);  // chunk, and scale, of the lane within a tile
+      int pg[4];
+      uint32_t place[4], there[4];
+      uint4 k[4], v[4];
+      uint32_t ks[4], vs[4];
+      auto look_up = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pg[i] = table[(uint32_t)min(p0 + 16 * i, end - 1) >> a.m.page_log2];
+      };
+      auto find = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t page = __builtin_amdgcn_readfirstlane(pg[i]);
+          const int q = p0 + 16 * i, n = page < (uint32_t)a.m.n_pages ? min(max(end - q, 0), 16) : 0;
+          place[i] = n > 0 ? page * a.page16 + (((uint32_t)kvh << a.m.page_log2) + ((uint32_t)q & in_page)) * 4 : 0;
+          there[i] = (1u << n) - 1;
+        }
+      };
+      look_up(mine);
+      find(mine);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        k[i] = (K + (size_t)place[i])[at];
+        ks[i] = (a.K_scale + (size_t)place[i])[at];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = (V + (size_t)place[i])[at];
+        vs[i] = (a.V_scale + (size_t)place[i])[at];
+      }
+      look_up(mine + kWaves * BN);
+      for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
+        const bool part = p0 + BN > least, more = p0 + kWaves * BN < end;
+        const bool whole = !part && (there[0] & there[1] & there[2] & there[3]) == 0xffffu;
+        uint32_t now[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) now[i] = there[i];
+        f32x4 s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = r.scores(k[i], ks[i]);
+        if (more) find(p0 + kWaves * BN);
+        if (more) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            k[i] = (K + (size_t)place[i])[at];
+            ks[i] = (a.K_scale + (size_t)place[i])[at];
+          }
+        }
+        if (!whole) {
+          asm volatile("");  // a branch: taken by few blocks
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.mask(s[i], p0 + 16 * i, now[i], lane);
+        }
+        uint4 x[2];
+        r.settle(s, c, x);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 code = v[2 * half + i];
+            const float f = scale_of(vs[2 * half + i]);
+            const uint32_t word[4] = {code.x, code.y, code.z, code.w};
+            const int row = 16 * i + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint4 y = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
+              if (!whole) {
+                if (!((now[2 * half + i] >> (lane & 15)) & 1)) y = make_uint4(0, 0, 0, 0);
+                if (part) {
+                  cleared |= odd<true>(y.x) || odd<true>(y.y) || odd<true>(y.z) || odd<true>(y.w);
+                  y = make_uint4(clear<true>(y.x), clear<true>(y.y), clear<true>(y.z), clear<true>(y.w));
+                }
+              }
+              *reinterpret_cast<uint4*>(vt + Rows16::chunk(row, 4 * (lane >> 4) + j)) = y;
+            }
+          }
+          if (half == 1 && more) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              v[i] = (V + (size_t)place[i])[at];
+              vs[i] = (a.V_scale + (size_t)place[i])[at];
+            }
+            look_up(p0 + 2 * kWaves * BN);
+          }
+          __builtin_amdgcn_wave_barrier();
+          r.output(vt, x[half], lane);
+        }
+      }
+    }
+    __syncthreads();  // (a state lies where other wavefronts' rows were)
+    float* const acc = reinterpret_cast<float*>(lds);
+    const int i = lane & 15, at = w * M + i;
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      *reinterpret_cast<f32x4*>(acc + (size_t)at * kD + 4 * ((4 * t + (lane >> 4)) ^ i)) = r.o[t];
+    const float sum = Rows16::sum_lanes(r.sum);
+    if (lane < 16) {
+      wm[at] = r.mx;
+      ws[at] = sum;
+    }
+    __syncthreads();
+    join_states<true>(a, p, kvh, rows, kWaves, M, acc, wm, ws);
+    if (__syncthreads_or(cleared))
+      add_left_out<true, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, kWaves, M);
+  }
+}
+
 // 33 to 64 rows: rows of the pool are read and decoded once for all of them, which a thin workgroup per 32 rows would do
 // twice.  Bound by the decoding and the barriers between blocks more than by memory.  1 to 5 tokens of 8 sequences of 7K to 64K,
 // 7 heads a group, i8, 192 MB: 64 us with the join, 3.0 TB/s (75 with pieces from the longest sequence alone: no more than 372 of the 512
@@ -1222,7 +1481,7 @@ constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 // 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
 // more in tiles.
 struct Cut {
-  int rows;  // 32: thin, 64: pair, 128: tile
+  int rows;  // 16: few, 32: thin, 64: pair, 128: tile
   int units, pieces, prefer, want, least;  // units: of a KV head, at most; the others: piece_of
 };
 Cut cut(const lrqk_pages_shape& s) {
@@ -1230,11 +1489,11 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t most = (int64_t)s.n_max * G;
   const bool f32 = s.kv_dtype == LRQK_KV_F32;
   Cut c;
-  c.rows = most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
+  c.rows = most <= 16 && s.page >= 16 && !f32 && s.page_dtype == LRQK_PAGE_E2M1 ? 16 : most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
   const int full = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows), tiles = full + s.B;  // sum_b ceil(n_b G / rows) is no more
   const int64_t units = (int64_t)std::max(s.B, full) * s.Hkv;
   // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
-  const int held = c.rows == 32 && f32 ? 256 : 512;
+  const int held = c.rows == 16 ? kFewWaves * 256 : c.rows == 32 && f32 ? 256 : 512;
   const int64_t state = (int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float);
   // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head would
   // be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not at the
@@ -1244,7 +1503,7 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t least = (s.l_max + c.least - 1) / c.least;  // pieces, with those
   c.prefer = 1;
   c.want = 0;
-  if (most <= 128 && s.B <= 4096 && (c.rows != 32 || f32)) {
+  if (most <= 128 && s.B <= 4096 && (c.rows > 32 || f32)) {
     // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
     // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 64 / 72 / 79; 12 tokens of 2 sequences of 32K
     // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234.  States of 64 MiB at most.
@@ -1294,11 +1553,13 @@ hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
 
 template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
-  const int most = std::max(1, kFewGrid / s.Hkv);
+  const int most = std::max(1, (c.rows == 16 ? kFewWaves * 256 : kFewGrid) / s.Hkv);
   const dim3 grid((unsigned)(s.Hkv * (c.rows == 128 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
   if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
-  else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
+  else if (c.rows == 16) {
+    if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) hipLaunchKernelGGL(attend_few_kernel, grid, dim3(kThreads), 0, st, a);
+  } else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
   else if (c.rows == 64) {
     if constexpr (BF16) hipLaunchKernelGGL((attend_pair_kernel<PAGE>), grid, dim3(kThreads), 0, st, a);
   } else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
