@@ -43,7 +43,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.0f;
 constexpr float kHeavy = 4096.0f;
 constexpr float kFar = 1073741824.0f;  // see Rows::weigh
-constexpr int kFewWaves = 2;           // wavefronts a SIMD of attend_few_kernel
 constexpr int kPartial = kPartialStride;  // floats of a partial state: max, sum, 2 unused, acc[128]
 
 struct Args {
@@ -353,12 +352,13 @@ struct Block {
     if constexpr (!coded(PAGE)) {
       o[0] = x;
     } else if constexpr (PAGE == LRQK_PAGE_E2M1) {
-      const float s = scale_of(byte);
       if constexpr (BF16) {
+        const float s = scale_bits(byte);
         const uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = decode8_bf16<PAGE>(w[j], s);
       } else {
+        const float s = scale_of(byte);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           float f[8];
@@ -1092,11 +1092,11 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
   }
 }
 
-// ---- 16 rows of the problem in a wavefront, pages of 4 bits --------------------------------------------------
-// Lane l: row l % 16; the 16 positions of a tile of S^T are 4 (l / 16) + v, v the register; elements of O^T likewise.  A row of
-// K goes straight from its load into the product: the sum over elements may run in any order, so that the lane that holds
-// 32 codes of a row, one block with one scale, multiplies them eight at a time with those eight of its q.
-struct Rows16 {
+// ---- 16 rows of the problem, or 32, in a wavefront: pages of 4 bits -------------------------------------------
+// Lane l: row l % 16 of a set; the 16 positions of a tile of S^T are 4 (l / 16) + v, v the register; elements of O^T likewise.
+// A row of K goes straight from its load into the product: the sum over elements may run in any order, so that the lane
+// that holds 32 codes of a row, one block with one scale, multiplies them eight at a time with those eight of its q.
+struct Set16 {
   uint4 q[4];   // elements 32 (l / 16) + 8 s .. + 7
   f32x4 o[8];   // elements 16 t ..
   float mx, sum;
@@ -1115,15 +1115,12 @@ struct Rows16 {
     mx = -INFINITY;
     sum = 0.0f;
   }
-  // scores of 16 positions: codes of row l % 16, block l / 16
-  __device__ __forceinline__ f32x4 scores(const uint4 codes, uint32_t byte) const {
-    const float f = scale_of(byte);
-    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+  // scores of 16 positions: a tile of K, row l % 16, block l / 16, eight elements each
+  __device__ __forceinline__ f32x4 scores(const uint4 (&tile)[4]) const {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, decode8_bf16<LRQK_PAGE_E2M1>(w[k], f)),
-                                                  __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, tile[k]), __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
     return s;
   }
   // scores of the 16 positions from p0 that the row does not see, or that are not there, become -infinity
@@ -1151,72 +1148,59 @@ struct Rows16 {
       for (int e = 0; e < 4; ++e) o[t][e] *= f;
     mx = to;
   }
-  // Weights of 64 positions (see Rows::weigh and weigh_any) as the second product's operands, 32 each, at a maximum that is
-  // raised where it has to be.
-  __device__ __forceinline__ void settle(const f32x4 (&s)[4], float c, uint4 (&x)[2]) {
+  // the largest score of 64 positions, in units of log2
+  static __device__ __forceinline__ float largest(const f32x4 (&s)[4], float c) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
-    top = over_lanes(top) * c;
-    if (__any(top > mx + kLag)) raise(top);
+    return over_lanes(top) * c;
+  }
+  // Weights of 64 positions (see Rows::weigh and weigh_any) as the second product's operands, 32 each.  far: some row's maximum is
+  // beyond kFar.
+  template <bool FAR>
+  __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, uint4 (&x)[2]) {
     const float base = mx == -INFINITY ? 0.0f : mx;
-    const auto form = [&](auto weight) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = weight(s[2 * i + e / 4][e % 4]);
-        x[i] = make_uint4(dev::pack_bf16(w[0], w[1]), dev::pack_bf16(w[2], w[3]), dev::pack_bf16(w[4], w[5]), dev::pack_bf16(w[6], w[7]));
-      }
-    };
-    form([&](float y) { return __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, -base)); });
-    if (__builtin_expect(__any(fabsf(mx) >= kFar), 0)) {
-      asm volatile("");  // a branch, which next to no call takes
-      const bool rounded = fabsf(mx) >= kFar;
-      form([&](float y) {
+    const bool rounded = FAR && fabsf(mx) >= kFar;
+    const auto weight = [&](float y) {
 #pragma clang fp contract(off)
+      if constexpr (FAR) {
         const float z = y * c;
         return __builtin_amdgcn_exp2f(rounded ? z - base : __builtin_fmaf(y, c, -base));
-      });
-    }
+      } else {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, -base));
+      }
+    };
     const dev::bf16x2 one = __builtin_bit_cast(dev::bf16x2, 0x3f803f80u);
-    float add = 0.0f;
+    float add[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      uint32_t w[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) add = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e]), one, add, false);
+      for (int e = 0; e < 4; ++e) {
+        w[e] = dev::pack_bf16(weight(s[2 * i + e / 2][2 * e % 4]), weight(s[2 * i + e / 2][2 * e % 4 + 1]));
+        add[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e]), one, add[i], false);
+      }
+      x[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    sum += add;
-  }
-  // O += weights of 32 positions times their V rows.  The weights' order: 4 (l / 16) + j, then 16 + 4 (l / 16) + j.
-  __device__ __forceinline__ void output(const char* vt, const uint4 x, int lane) {
-    const int g = lane & 15, row = 4 * (lane >> 4) + (g >> 2);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      s16x4 v[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(vt + chunk(row + 16 * j, 2 * t + ((g & 3) >> 1)) + 8 * (g & 1)));
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), __builtin_bit_cast(bf16x8, x), o[t], 0, 0, 0);
-    }
-  }
-  // Where LDS holds chunk c of a row: eight rows' same chunk (as they are stored) lies in eight places mod 8, eight rows' two
-  // chunks (as they are read) in sixteen.
-  static __device__ __forceinline__ int chunk(int row, int c) {
-    return row * kRowB<true> + ((c ^ (((row & 7) << 1) | ((row >> 2) & 1))) << 4);
+    sum += add[0] + add[1];
   }
 };
+// Where LDS holds chunk c of a row of V: eight rows' same chunk (as they are stored) lies in eight places mod 8, eight rows' two
+// chunks (as they are read) in sixteen.
+__device__ __forceinline__ int few_chunk(int row, int c) {
+  return row * kRowB<true> + ((c ^ (((row & 7) << 1) | ((row >> 2) & 1))) << 4);
+}
 
-// At most 16 rows a workgroup, pages of 4 bits: a wavefront takes every fourth block of 64 positions, four tiles of 16, each of
-// which lies in one page.  K does not touch LDS; V passes through 8 KB of it, 32 positions at a time.
-__global__ __launch_bounds__(kThreads, kFewWaves) void attend_few_kernel(const Args a) {
-  constexpr int M = 16, BN = 64, kTile = 32 * kRowB<true>;
-  __shared__ __align__(16) char lds[kWaves * kTile];
+// At most 16 NS rows a workgroup, pages of 4 bits: a wavefront takes every fourth block of 64 positions, four tiles of 16, each of
+// which lies in one page.  K does not touch LDS; V passes through 16 KB of it.  Two sets of rows share the
+// decoded tiles; both are always worked on (with code of its own for units that have one set of rows only, 180 bytes of registers spilled
+// and the whole took 1.6 to 2 times as long), and the maximum is looked at for both together.
+template <int NS>
+__global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
+  constexpr int M = 16 * NS, BN = 64, kTile = BN * kRowB<true>, kStep = kWaves * BN;
+  __shared__ __align__(16) char lds[kWaves * kTile];  // a wavefront's rows of V; then the states
   __shared__ float wm[kWaves * M], ws[kWaves * M];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % a.m.Hkv;
@@ -1226,15 +1210,18 @@ __global__ __launch_bounds__(kThreads, kFewWaves) void attend_few_kernel(const A
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
     Problem p;
-    if (!find_unit<M, false>(a, unit, p)) return;
+    if (!find_unit<M, true>(a, unit, p)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
     const int from = p.piece * p.step, end = min(most, from + p.step);
     if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
-    Rows16 r;
-    const int real = min(p.r0 + (lane & 15), p.rows - 1);
-    r.see = sees(a, p, real);
-    r.start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    Set16 r[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const int real = min(p.r0 + 16 * n + (lane & 15), p.rows - 1);
+      r[n].see = sees(a, p, real);
+      r[n].start(a.q, (int64_t)(p.s.first + real / a.G) * (a.m.Hkv * a.G) + kvh * a.G + real % a.G, a.scale < 0.0f, lane);
+    }
     const float c = log2_scale(a);
     char* const vt = lds + w * kTile;
     bool cleared = false;
@@ -1260,88 +1247,126 @@ __global__ __launch_bounds__(kThreads, kFewWaves) void attend_few_kernel(const A
           there[i] = (1u << n) - 1;
         }
       };
+      auto fetch = [&](const uint4* base, const uint8_t* scale, uint4 (&x)[4], uint32_t (&y)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = (base + (size_t)place[i])[at];
+          y[i] = (scale + (size_t)place[i])[at];  // (a row is four chunks and has four scales)
+        }
+      };
       look_up(mine);
       find(mine);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        k[i] = (K + (size_t)place[i])[at];
-        ks[i] = (a.K_scale + (size_t)place[i])[at];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = (V + (size_t)place[i])[at];
-        vs[i] = (a.V_scale + (size_t)place[i])[at];
-      }
-      look_up(mine + kWaves * BN);
-      for (int p0 = mine; p0 < end; p0 += kWaves * BN) {
-        const bool part = p0 + BN > least, more = p0 + kWaves * BN < end;
+      fetch(K, a.K_scale, k, ks);
+      fetch(V, a.V_scale, v, vs);
+      look_up(mine + kStep);
+      bool far = false;
+      for (int p0 = mine; p0 < end; p0 += kStep) {
+        const bool part = p0 + BN > least, more = p0 + kStep < end;
         const bool whole = !part && (there[0] & there[1] & there[2] & there[3]) == 0xffffu;
         uint32_t now[4];
+        // V into LDS, all 64 positions, long before it is read
+        __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
 #pragma unroll
-        for (int i = 0; i < 4; ++i) now[i] = there[i];
-        f32x4 s[4];
+        for (int i = 0; i < 4; ++i) {
+          now[i] = there[i];
+          const float f = scale_bits(vs[i]);
+          const uint32_t word[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = r.scores(k[i], ks[i]);
-        if (more) find(p0 + kWaves * BN);
-        if (more) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            k[i] = (K + (size_t)place[i])[at];
-            ks[i] = (a.K_scale + (size_t)place[i])[at];
+          for (int j = 0; j < 4; ++j) {
+            uint4 y = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
+            if (!whole) {
+              if (!((now[i] >> (lane & 15)) & 1)) y = make_uint4(0, 0, 0, 0);
+              if (part) {
+                cleared |= odd<true>(y.x) || odd<true>(y.y) || odd<true>(y.z) || odd<true>(y.w);
+                y = make_uint4(clear<true>(y.x), clear<true>(y.y), clear<true>(y.z), clear<true>(y.w));
+              }
+            }
+            *reinterpret_cast<uint4*>(vt + few_chunk(16 * i + (lane & 15), 4 * (lane >> 4) + j)) = y;
           }
         }
+        if (more) {
+          find(p0 + kStep);
+          fetch(V, a.V_scale, v, vs);
+        }
+        f32x4 s[NS][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = scale_bits(ks[i]);
+          const uint32_t word[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+          uint4 tile[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) tile[j] = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
+#pragma unroll
+          for (int n = 0; n < NS; ++n) s[n][i] = r[n].scores(tile);
+        }
+        if (more) {
+          fetch(K, a.K_scale, k, ks);
+          look_up(p0 + 2 * kStep);
+        }
+        __builtin_amdgcn_wave_barrier();
+        float top[NS];
+        bool raise = false;
         if (!whole) {
           asm volatile("");  // a branch: taken by few blocks
 #pragma unroll
-          for (int i = 0; i < 4; ++i) r.mask(s[i], p0 + 16 * i, now[i], lane);
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[n].mask(s[n][i], p0 + 16 * i, now[i], lane);
         }
-        uint4 x[2];
-        r.settle(s, c, x);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          top[n] = Set16::largest(s[n], c);
+          raise |= top[n] > r[n].mx + kLag;
+        }
+        if (__any(raise)) {
+          bool beyond = false;
+#pragma unroll
+          for (int n = 0; n < NS; ++n) {
+            r[n].raise(top[n]);
+            beyond |= fabsf(r[n].mx) >= kFar && r[n].mx != -INFINITY;
+          }
+          far = __any(beyond);
+        }
+        uint4 x[NS][2];
+        if (__builtin_expect(far, 0)) {
+#pragma unroll
+          for (int n = 0; n < NS; ++n) r[n].template weigh<true>(s[n], c, x[n]);
+        } else {
+#pragma unroll
+          for (int n = 0; n < NS; ++n) r[n].template weigh<false>(s[n], c, x[n]);
+        }
+        // the weights' order: 4 (l / 16) + j, then 16 + 4 (l / 16) + j
+        const int g = lane & 15, row = 4 * (lane >> 4) + (g >> 2);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 code = v[2 * half + i];
-            const float f = scale_of(vs[2 * half + i]);
-            const uint32_t word[4] = {code.x, code.y, code.z, code.w};
-            const int row = 16 * i + (lane & 15);
+          for (int t = 0; t < 8; ++t) {
+            s16x4 y[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint4 y = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
-              if (!whole) {
-                if (!((now[2 * half + i] >> (lane & 15)) & 1)) y = make_uint4(0, 0, 0, 0);
-                if (part) {
-                  cleared |= odd<true>(y.x) || odd<true>(y.y) || odd<true>(y.z) || odd<true>(y.w);
-                  y = make_uint4(clear<true>(y.x), clear<true>(y.y), clear<true>(y.z), clear<true>(y.w));
-                }
-              }
-              *reinterpret_cast<uint4*>(vt + Rows16::chunk(row, 4 * (lane >> 4) + j)) = y;
-            }
+            for (int j = 0; j < 2; ++j)
+              y[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+                  vt + few_chunk(row + 16 * j + 32 * half, 2 * t + ((g & 3) >> 1)) + 8 * (g & 1)));
+            const bf16x8 z = __builtin_bit_cast(bf16x8, __builtin_shufflevector(y[0], y[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+              r[n].o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z, __builtin_bit_cast(bf16x8, x[n][half]), r[n].o[t], 0, 0, 0);
           }
-          if (half == 1 && more) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              v[i] = (V + (size_t)place[i])[at];
-              vs[i] = (a.V_scale + (size_t)place[i])[at];
-            }
-            look_up(p0 + 2 * kWaves * BN);
-          }
-          __builtin_amdgcn_wave_barrier();
-          r.output(vt, x[half], lane);
         }
       }
     }
     __syncthreads();  // (a state lies where other wavefronts' rows were)
     float* const acc = reinterpret_cast<float*>(lds);
-    const int i = lane & 15, at = w * M + i;
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      *reinterpret_cast<f32x4*>(acc + (size_t)at * kD + 4 * ((4 * t + (lane >> 4)) ^ i)) = r.o[t];
-    const float sum = Rows16::sum_lanes(r.sum);
-    if (lane < 16) {
-      wm[at] = r.mx;
-      ws[at] = sum;
+    for (int n = 0; n < NS; ++n) {
+      const int i = 16 * n + (lane & 15), to = w * M + i;
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        *reinterpret_cast<f32x4*>(acc + (size_t)to * kD + 4 * ((4 * t + (lane >> 4)) ^ i)) = r[n].o[t];
+      const float sum = Set16::sum_lanes(r[n].sum);
+      if (lane < 16) {
+        wm[to] = r[n].mx;
+        ws[to] = sum;
+      }
     }
     __syncthreads();
     join_states<true>(a, p, kvh, rows, kWaves, M, acc, wm, ws);
@@ -1474,6 +1499,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
+constexpr int kFewRows = 64;   // rows of the problem up to which pages of 4 bits are attended to by attend_few_kernel
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
 // How a call is cut up.  At most 32 rows a sequence and KV head go the thin way, and all calls with pages of less than 16
@@ -1481,7 +1507,8 @@ constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 // 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
 // more in tiles.
 struct Cut {
-  int rows;  // 16: few, 32: thin, 64: pair, 128: tile
+  int rows;  // 16: few, 32: few or thin, 64: pair, 128: tile
+  bool few;
   int units, pieces, prefer, want, least;  // units: of a KV head, at most; the others: piece_of
 };
 Cut cut(const lrqk_pages_shape& s) {
@@ -1489,21 +1516,22 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t most = (int64_t)s.n_max * G;
   const bool f32 = s.kv_dtype == LRQK_KV_F32;
   Cut c;
-  c.rows = most <= 16 && s.page >= 16 && !f32 && s.page_dtype == LRQK_PAGE_E2M1 ? 16 : most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
+  c.few = s.page_dtype == LRQK_PAGE_E2M1 && !f32 && s.page >= 16 && most <= kFewRows;
+  c.rows = c.few ? (most <= 16 ? 16 : 32) : most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
   const int full = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows), tiles = full + s.B;  // sum_b ceil(n_b G / rows) is no more
   const int64_t units = (int64_t)std::max(s.B, full) * s.Hkv;
   // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
-  const int held = c.rows == 16 ? kFewWaves * 256 : c.rows == 32 && f32 ? 256 : 512;
+  const int held = c.rows == 32 && f32 ? 256 : 512;
   const int64_t state = (int64_t)s.T * s.Hq * kPartial * (int64_t)sizeof(float);
   // In a batch there may be sequences of few new tokens and a long context among the others, which a workgroup a head would
   // be left with (a chunk of 4096 and seven single tokens at 120K: 1073 us, and 818 with pieces of 16384).  Not at the
   // price of partial states of more than a gigabyte.
   const int64_t few = s.B > 1 ? std::min<int64_t>((s.l_max + 16383) / 16384, (1ll << 30) / state) : 1;
-  c.least = most > 128 ? 512 : s.B > 1 ? 256 : 128;
+  c.least = most > 128 ? 512 : s.B > 1 || c.few ? 256 : 128;
   const int64_t least = (s.l_max + c.least - 1) / c.least;  // pieces, with those
   c.prefer = 1;
   c.want = 0;
-  if (most <= 128 && s.B <= 4096 && (c.rows > 32 || f32)) {
+  if (most <= 128 && s.B <= 4096 && (c.rows > 32 || f32 || c.few)) {
     // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
     // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 64 / 72 / 79; 12 tokens of 2 sequences of 32K
     // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234.  States of 64 MiB at most.
@@ -1553,12 +1581,15 @@ hipError_t launch_thin(const dim3 grid, const Args& a, hipStream_t st) {
 
 template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
-  const int most = std::max(1, (c.rows == 16 ? kFewWaves * 256 : kFewGrid) / s.Hkv);
+  const int most = std::max(1, kFewGrid / s.Hkv);
   const dim3 grid((unsigned)(s.Hkv * (c.rows == 128 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
   if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
-  else if (c.rows == 16) {
-    if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) hipLaunchKernelGGL(attend_few_kernel, grid, dim3(kThreads), 0, st, a);
+  else if (c.few) {
+    if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) {
+      if (c.rows == 16) hipLaunchKernelGGL(attend_few_kernel<1>, grid, dim3(kThreads), 0, st, a);
+      else hipLaunchKernelGGL(attend_few_kernel<2>, grid, dim3(kThreads), 0, st, a);
+    }
   } else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
   else if (c.rows == 64) {
     if constexpr (BF16) hipLaunchKernelGGL((attend_pair_kernel<PAGE>), grid, dim3(kThreads), 0, st, a);

@@ -66,6 +66,10 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7fc00000u : x);
 }
 
+// The scale as the conversion from e2m1 to bf16 takes it: it looks at the exponent alone, where 0 is 2^-127 and 255 NaN (all codes
+// under all 256 bytes come out as with scale_of).
+__device__ __forceinline__ float scale_bits(uint32_t byte) { return __uint_as_float(byte << 23); }
+
 // Eight codes times their scale, in fp32 (exact).
 template <int PAGE>
 __device__ __forceinline__ void decode8(Codes8<PAGE> c, float s, float (&x)[8]) {
