@@ -541,18 +541,23 @@ _KV_TYPES = {torch.bfloat16: LRQK_KV_BF16, torch.float32: LRQK_KV_F32}
 
 def _heads(t: torch.Tensor, T: int):
     """Pointer, heads, type and stride of rows [T,heads,128], each token's dense; tokens may lie further apart."""
+    if t.dim() != 3:
+        raise ValueError(f"expected [{T}, heads, 128], got {tuple(t.shape)}")
+    n, heads, d = t.shape
+    apart, head, one = t.stride()
+    kind = _KV_TYPES.get(t.dtype)
+    if T == 1:
+        apart = heads * 128
+    if (t.is_cuda and kind is not None and n == T and d == 128 and one == 1 and (head == 128 or heads == 1)
+            and heads * 128 <= apart < 1 << 31):
+        return t.data_ptr(), heads, kind, apart
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
-    kind = _KV_TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"rows of {t.dtype}")
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != 128:
+    if n != T or d != 128:
         raise ValueError(f"expected [{T}, heads, 128], got {tuple(t.shape)}")
-    apart, head, one = t.stride()
-    dense = t.shape[1] * 128
-    if one != 1 or (head != 128 and t.shape[1] > 1) or (T > 1 and not dense <= apart < 1 << 31):
-        raise ValueError(f"rows of a token are not dense, or tokens overlap: strides {t.stride()}")
-    return t.data_ptr(), t.shape[1], kind, apart if T > 1 else 0
+    raise ValueError(f"rows of a token are not dense, or tokens overlap: strides {t.stride()}")
 
 
 def _here(stream, rope: Rope, *tensors):
@@ -566,24 +571,25 @@ def _here(stream, rope: Rope, *tensors):
     return torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
 
 
+_NO_ROWS = (None, 0, 0, 0)
+
+
 def lrqk_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, stream=None):
     """q, q_out [T,Hq,128] and k, k_out [T,Hkv,128], tokens as far apart as their strides say; pos [T] int32."""
     T = pos.numel()
-    s = RotateShape(T=T, d=128)
-    ptr = [None, None, None, None]
-    if q is not None and q_out is not None:
-        ptr[0], s.Hq, s.q_type, s.q_stride = _heads(q, T)
-        ptr[1], heads, s.q_out_type, s.q_out_stride = _heads(q_out, T)
-        if heads != s.Hq:
-            raise ValueError(f"q of {s.Hq} heads, q_out of {heads}")
-    if k is not None and k_out is not None:
-        ptr[2], s.Hkv, s.k_type, s.k_stride = _heads(k, T)
-        ptr[3], heads, kind, s.k_out_stride = _heads(k_out, T)
-        if heads != s.Hkv or kind != s.k_type:
-            raise ValueError(f"k {tuple(k.shape)} of {k.dtype}, k_out {tuple(k_out.shape)} of {k_out.dtype}")
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("an input without its output, or an output without its input")
-    _check(load_library().lrqk_rotate(C.byref(s), C.byref(rope), _dev(pos, torch.int32), *ptr,
+    a = b = x = y = _NO_ROWS
+    if q is not None:
+        a, b = _heads(q, T), _heads(q_out, T)
+        if a[1] != b[1]:
+            raise ValueError(f"q of {a[1]} heads, q_out of {b[1]}")
+    if k is not None:
+        x, y = _heads(k, T), _heads(k_out, T)
+        if x[1:3] != y[1:3]:
+            raise ValueError(f"k {tuple(k.shape)} of {k.dtype}, k_out {tuple(k_out.shape)} of {k_out.dtype}")
+    s = RotateShape(T, a[1], x[1], 128, a[2], b[2], x[2], a[3], b[3], x[3], y[3])
+    _check(load_library().lrqk_rotate(C.byref(s), C.byref(rope), _dev(pos, torch.int32), a[0], b[0], x[0], y[0],
                                       _here(stream, rope, pos, q, q_out, k, k_out)), "lrqk_rotate")
 
 
@@ -591,26 +597,28 @@ def lrqk_pages_rotate_append(shape, pages, rope: Rope, q, k_new, v_new, q_out, p
     """q [T,Hq,128], k_new, v_new [T,Hkv,128] of shape.kv_dtype, tokens as far apart as their strides say; q_out dense.
     q and q_out may both be None; pos and slot [T] int32 both or neither."""
     _hold(pages, shape)
-    n, T = NewRows(), shape.T
+    T, kind = shape.T, shape.kv_dtype
     if (q is None) != (q_out is None) or (pos is None) != (slot is None):
         raise ValueError("q without q_out or pos without slot, or the other way round")
-    kinds = []
+    a, out = _NO_ROWS, None
     if q is not None:
-        n.q, heads, kind, n.q_stride = _heads(q, T)
-        if heads != shape.Hq:
-            raise ValueError(f"q of {heads} heads, Hq = {shape.Hq}")
-        kinds.append(kind)
-        n.q_out = _fits(q_out, shape, T * shape.Hq)
-    n.k, heads, kind, n.k_stride = _heads(k_new, T)
-    n.v, heads_v, kind_v, n.v_stride = _heads(v_new, T)
-    if heads != shape.Hkv or heads_v != shape.Hkv:
-        raise ValueError(f"k of {heads} heads and v of {heads_v}, Hkv = {shape.Hkv}")
-    if any(x != shape.kv_dtype for x in kinds + [kind, kind_v]):
-        raise TypeError(f"rows of another type than kv_dtype {shape.kv_dtype}")
+        a = _heads(q, T)
+        if a[1] != shape.Hq:
+            raise ValueError(f"q of {a[1]} heads, Hq = {shape.Hq}")
+        if a[2] != kind:
+            raise TypeError(f"q of {q.dtype}, kv_dtype {kind}")
+        out = _fits(q_out, shape, T * shape.Hq)
+    k, v = _heads(k_new, T), _heads(v_new, T)
+    if k[1] != shape.Hkv or v[1] != shape.Hkv:
+        raise ValueError(f"k of {k[1]} heads and v of {v[1]}, Hkv = {shape.Hkv}")
+    if k[2] != kind or v[2] != kind:
+        raise TypeError(f"k of {k_new.dtype} and v of {v_new.dtype}, kv_dtype {kind}")
+    at = to = None
     if pos is not None:
         if pos.numel() < T or slot.numel() < T:
             raise ValueError(f"expected {T} positions and slots, got {pos.numel()} and {slot.numel()}")
-        n.pos, n.slot = _dev(pos, torch.int32), _dev(slot, torch.int32)
+        at, to = _dev(pos, torch.int32), _dev(slot, torch.int32)
+    n = NewRows(a[0], k[0], v[0], a[3], k[3], v[3], out, at, to)
     st = _raw_stream(stream, pages, q, k_new, v_new, q_out, pos, slot)
     if getattr(rope, "tensor", None) is not None and rope.tensor.get_device() != k_new.get_device():
         raise ValueError(f"rope on {rope.tensor.device}, rows on {k_new.device}")
