@@ -16,7 +16,9 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kSeqs = 2048;           // sequences whose numbers LDS holds
 constexpr int kTile = kThreads * 16;  // pages looked at together: a wavefront takes 1024 of them, four loads of four a lane
-constexpr int kRowsHere = 4096;       // rows whose maps the one workgroup makes; with more a second launch is shorter
+// Rows whose maps the one workgroup makes (256 sequences, 4096 rows: 13.0 us, and 15.1 with a launch of their own; 8448: 16.3 and 15.9).
+constexpr int kRowsHere = 6144;
+constexpr int kSmall = 2;  // pages of a sequence that its own thread gives back or takes
 // Pages whose counts the one workgroup looks through: 64K of them take it 4.5 us, and two launches 5 however many there are.
 constexpr int kPagesHere = 4 * kTile;
 
@@ -103,10 +105,41 @@ __device__ __forceinline__ uint32_t in_wave(uint32_t mask, uint32_t (&before)[4]
   return n;
 }
 
-__device__ __forceinline__ void put_maps(const Args& a, int t, int b, int pos, int page) {
-  if (a.seq) a.seq[t] = b;
-  if (a.pos) a.pos[t] = pos;
-  if (a.slot) a.slot[t] = (unsigned)page >= (unsigned)a.n_pages ? -1 : (page << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
+// The maps of rows t0 .. t0 + 3.  `at(b)`: what a row's number has to be added to for its position.  Found with one search: the
+// rows after the first are its sequence's or those of one of the next.
+template <typename F>
+__device__ __forceinline__ void put_maps(const Args& a, int t0, const int32_t* start, int n_rows, F at) {
+  int b[4], pos[4], pg[4];
+  int s = t0 < n_rows ? last_upto(start, a.B, t0) : 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int t = t0 + j;
+    b[j] = pos[j] = pg[j] = -1;
+    if (t < n_rows) {
+      for (int i = 0; t >= start[s + 1]; ++i) s = i < 2 ? s + 1 : last_upto(start, a.B, t);
+      b[j] = s;
+      pos[j] = at(s) + t;
+    }
+  }
+  if (a.slot) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (b[j] >= 0) pg[j] = a.table[(size_t)b[j] * a.max_pages + (pos[j] >> a.page_log2)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      pg[j] = (unsigned)pg[j] >= (unsigned)a.n_pages ? -1 : (pg[j] << a.page_log2) + (pos[j] & ((1 << a.page_log2) - 1));
+  }
+  auto put = [&](int32_t* map, const int (&x)[4]) {
+    if (!map) return;
+    if (t0 + 4 <= a.T) {
+      *reinterpret_cast<int4*>(map + t0) = make_int4(x[0], x[1], x[2], x[3]);
+    } else {
+      for (int j = 0; j < 4 && t0 + j < a.T; ++j) map[t0 + j] = x[j];
+    }
+  };
+  put(a.seq, b);
+  put(a.pos, pos);
+  put(a.slot, pg);
 }
 
 // Positions kept of b's `old`.
@@ -141,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   __shared__ int32_t lds[LDS ? 4 * (kSeqs + 1) : 1];
   __shared__ uint16_t pick[kTile];  // free pages of a tile, ascending
   __shared__ Totals tot;
-  __shared__ int32_t most, first_tile;
+  __shared__ int32_t most, first_tile, big;
   const int size = LDS ? kSeqs + 1 : a.B + 1;
   int32_t* const kept = LDS ? lds : a.work;  // [B] positions kept
   int32_t* const want = kept + size;         // [B] new tokens, or -status
@@ -150,8 +183,9 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, page = 1 << a.page_log2;
   int turn = 0;
 
-  // 1: cut back.  Each thread takes entries that are given back wherever they are: a loop over a sequence's would wait for
-  // one load after the other (28 us instead of 10 for 256 sequences, of which a third give something back).
+  // 1: cut back.  A sequence's thread gives back a page or two; the entries of those that give back more are dealt out to
+  // all threads, since a loop over a sequence's would wait for one load after the other (256 sequences, of which a third give something
+  // back: 28 us with such loops).
   uint64_t gone = 0;
   int last = -1;  // the page of position `kept`, if that is no page's first (one sequence a thread: looked up on the way)
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
@@ -164,7 +198,19 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
       n_gone = a.counts ? 0 : pages_of(a, old) - pages_of(a, k);
       kept[b] = k;
       want[b] = n > 0 && (n > a.n_max || n > a.l_max - k) ? -LRQK_ADVANCE_LONG : n;
-      if ((k & (page - 1)) != 0) last = a.table[(size_t)b * a.max_pages + (k >> a.page_log2)];
+      int32_t* const row = a.table + (size_t)b * a.max_pages;
+      if ((k & (page - 1)) != 0) last = row[k >> a.page_log2];
+      if (n_gone <= kSmall) {
+        int pg[kSmall];
+#pragma unroll
+        for (int i = 0; i < kSmall; ++i) pg[i] = i < n_gone ? row[pages_of(a, k) + i] : -1;
+#pragma unroll
+        for (int i = 0; i < kSmall; ++i) {
+          if (i < n_gone) row[pages_of(a, k) + i] = -1;
+          if ((unsigned)pg[i] < (unsigned)a.n_pages) atomicSub(a.refs + pg[i], 1);
+        }
+        n_gone = 0;
+      }
     }
     const Sums s = scan((uint32_t)n_gone, 0u, tot, turn);
     if (b < a.B) rank[b] = (int32_t)min(gone + s.x, (uint64_t)INT32_MAX);
@@ -172,6 +218,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   }
   if (threadIdx.x == 0) {
     most = 0;
+    big = 0;
     first_tile = INT32_MAX;
   }
   __syncthreads();
@@ -200,6 +247,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
       }
       need = n > 0 ? pages_of(a, k + n) - pages_of(a, k) : 0;
       n = max(n, 0);
+      if (need > kSmall) big = 1;
     }
     const Sums s = scan((uint32_t)need, (uint32_t)n, tot, turn);
     if (b < a.B) {
@@ -289,7 +337,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   }
   __syncthreads();
 
-  // 3: the pages: a tile's free ones in order, then a thread for each that is given away
+  // 3: the pages: a tile's free ones in order; a sequence's thread takes a page or two, a thread for each those of the others
   const int give = most;
   int64_t found = 0;
   for (int64_t base = from; base < a.n_pages && found < give; base += kTile) {
@@ -307,34 +355,33 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
         if (mask >> (4 * i + j) & 1) pick[r++] = (uint16_t)(w * 1024 + 256 * i + 4 * lane + j);
     }
     __syncthreads();
-    const int n = (int)min((int64_t)in_tile, give - found);
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const int r = (int)found + i, pg = (int)base + pick[i];
-      const int b = last_upto(rank, a.B, r);
-      a.refs[pg] = 1;
-      a.table[(size_t)b * a.max_pages + pages_of(a, kept[b]) + (r - rank[b])] = pg;
+    const int n = (int)min((int64_t)in_tile, give - found);  // of this tile
+    for (int b = threadIdx.x; b < a.B; b += kThreads) {
+      const int need = want[b] > 0 ? pages_of(a, kept[b] + want[b]) - pages_of(a, kept[b]) : 0;
+#pragma unroll
+      for (int i = 0; i < kSmall; ++i) {
+        const int64_t r = rank[b] + i - found;
+        if (need > kSmall || i >= need || r < 0 || r >= n) continue;
+        const int pg = (int)base + pick[r];
+        a.refs[pg] = 1;
+        a.table[(size_t)b * a.max_pages + pages_of(a, kept[b]) + i] = pg;
+      }
+    }
+    if (big) {
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const int r = (int)found + i, pg = (int)base + pick[i];
+        const int b = last_upto(rank, a.B, r), first = pages_of(a, kept[b]);
+        if (pages_of(a, kept[b] + want[b]) - first <= kSmall) continue;
+        a.refs[pg] = 1;
+        a.table[(size_t)b * a.max_pages + first + (r - rank[b])] = pg;
+      }
     }
     found += (int64_t)in_tile;
     __syncthreads();
   }
   if (!a.maps) return;
-  const int n_rows = start[a.B];
-  for (int t0 = threadIdx.x; t0 < a.T; t0 += 4 * kThreads) {
-    int b[4], pos[4], pg[4];  // together, not one after the other
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = t0 + i * kThreads;
-      b[i] = pos[i] = pg[i] = -1;
-      if (t < n_rows) {
-        b[i] = last_upto(start, a.B, t);
-        pos[i] = kept[b[i]] + (t - start[b[i]]);
-        if (a.slot) pg[i] = a.table[(size_t)b[i] * a.max_pages + (pos[i] >> a.page_log2)];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t0 + i * kThreads < a.T) put_maps(a, t0 + i * kThreads, b[i], pos[i], pg[i]);
-  }
+  for (int t = 4 * threadIdx.x; t < a.T; t += 4 * kThreads)
+    put_maps(a, t, start, start[a.B], [&](int i) { return kept[i] - start[i]; });
 }
 
 // The maps of many rows, from the tables.
@@ -347,16 +394,8 @@ __global__ __launch_bounds__(kMapThreads) void maps_kernel(const Args a) {
     __syncthreads();
     start = lds;
   }
-  const int n_rows = start[a.B];
-  for (int t = blockIdx.x * kMapThreads + threadIdx.x; t < a.T; t += gridDim.x * kMapThreads) {
-    if (t >= n_rows) {
-      put_maps(a, t, -1, -1, -1);
-      continue;
-    }
-    const int b = last_upto(start, a.B, t);
-    const int pos = a.kv_len[b] - start[b + 1] + t;  // kv_len - n + (t - start[b])
-    put_maps(a, t, b, pos, a.slot ? a.table[(size_t)b * a.max_pages + (pos >> a.page_log2)] : 0);
-  }
+  for (int t = 4 * (blockIdx.x * kMapThreads + threadIdx.x); t < a.T; t += 4 * gridDim.x * kMapThreads)
+    put_maps(a, t, start, start[a.B], [&](int i) { return a.kv_len[i] - start[i + 1]; });
 }
 
 __global__ __launch_bounds__(kMapThreads) void tables_init_kernel(const Args a) {
@@ -431,7 +470,7 @@ LRQK_API int lrqk_pages_advance(const lrqk_pages_shape* shape, const lrqk_pages_
   if (a.B <= kSeqs) hipLaunchKernelGGL(advance_kernel<true>, dim3(1), dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(advance_kernel<false>, dim3(1), dim3(kThreads), 0, st, a);
   if (any && !a.maps)
-    hipLaunchKernelGGL(maps_kernel, dim3((unsigned)std::min(ceil_div(a.T, kMapThreads), 2048)), dim3(kMapThreads), 0, st, a);
+    hipLaunchKernelGGL(maps_kernel, dim3((unsigned)std::min(ceil_div(a.T, 4 * kMapThreads), 2048)), dim3(kMapThreads), 0, st, a);
   LRQK_HIP(hipGetLastError());
   return LRQK_OK;
 }
