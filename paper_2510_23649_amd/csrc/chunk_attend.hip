@@ -145,15 +145,16 @@ __device__ __forceinline__ int piece_of(const Args& a, Seq s) {
 }
 
 // Unit `unit` of the work of a KV head: a sequence's units are its pieces, last one first, a piece's its tiles (M rows
-// each).  False if there are not that many.  Every wavefront finds it for itself, 64 sequences at a time.
-template <int M, bool EVEN>
-__device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
+// each).  False if there are not that many.  Every wavefront finds it for itself, 64 sequences at a time; p.step is given.
+// q: sequences from.i0 + lane.  Where the unit was found is left in `from`, for a later one to begin there.
+struct Cursor {
+  int i0, before;  // first of 64 sequences; units of those before them
+};
+template <int M>
+__device__ __forceinline__ bool find_from(const Args& a, int unit, Problem& p, Seq q, Cursor& from) {
   const int lane = threadIdx.x & 63;
-  Seq q = lane_sequence(a, 0);
-  p.step = piece_of<EVEN>(a, q);
-  int before = 0;
-  for (int i0 = 0; i0 < a.m.B; i0 += 64) {
-    if (i0 > 0) q = lane_sequence(a, i0);
+  int before = from.before;
+  for (int i0 = from.i0;;) {
     const int tiles = (q.n * a.G + M - 1) / M, pieces = max(1, (min(q.len, a.m.l_max) + p.step - 1) / p.step);
     const int units = i0 + lane < a.m.B ? tiles * pieces : 0;
     const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)units);
@@ -172,11 +173,21 @@ __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
       const int back = __builtin_amdgcn_readlane(units, j) - 1 - mine;
       p.piece = back / t;
       p.r0 = (back - p.piece * t) * M;
+      from = Cursor{i0, before};
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
+    i0 += 64;
+    if (i0 >= a.m.B) return false;
+    q = lane_sequence(a, i0);
   }
-  return false;
+}
+template <int M, bool EVEN>
+__device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
+  const Seq q = lane_sequence(a, 0);
+  p.step = piece_of<EVEN>(a, q);
+  Cursor from{0, 0};
+  return find_from<M>(a, unit, p, q, from);
 }
 
 // Positions that a row of the problem sees: [0, result).
@@ -1206,11 +1217,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
   const int kvh = blockIdx.x % a.m.Hkv;
   const uint4* const K = static_cast<const uint4*>(a.K);
   const uint4* const V = static_cast<const uint4*>(a.V);
+  Problem p;
+  Cursor cursor{0, 0};
+  Seq first = lane_sequence(a, 0);
+  p.step = piece_of<true>(a, first);
   for (int unit = blockIdx.x / a.m.Hkv;; unit += gridDim.x / a.m.Hkv) {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // what follows from it is made anew for a unit, and not kept in registers over all
-    Problem p;
-    if (!find_unit<M, true>(a, unit, p)) return;
+    if (!find_from<M>(a, unit, p, unit < gridDim.x / a.m.Hkv ? first : lane_sequence(a, cursor.i0), cursor)) return;
     const int rows = min(M, p.rows - p.r0);
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
     const int from = p.piece * p.step, end = min(most, from + p.step);
@@ -1370,6 +1384,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
     }
     __syncthreads();
     join_states<true>(a, p, kvh, rows, kWaves, M, acc, wm, ws);
+    if (a.partials && p.piece == 0 && (int)threadIdx.x < rows) {  // what attend_join_few_kernel goes by
+      const int row = p.r0 + threadIdx.x;
+      const int64_t at = (int64_t)(p.s.first + row / a.G) * (a.m.Hkv * a.G) + kvh * a.G + row % a.G;
+      a.partials[at * a.pieces * kPartial + 2] = __int_as_float(max(1, (most + p.step - 1) / p.step));
+    }
     if (__syncthreads_or(cleared))
       add_left_out<true, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, kWaves, M);
   }
@@ -1499,6 +1518,79 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
   else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
+// The same for attend_few_kernel's states: the number of a row's pieces stands with its first one, so that a row asks for
+// everything at once, its first states before it knows how many there are, and nothing depends on the number of sequences (a
+// token of 256 sequences, 8192 rows: 101 us in attend_join_kernel, where every row looks through their lengths).  W wavefronts a row:
+// all of them weigh all pieces, each adds up every W-th.
+template <int W>
+__global__ __launch_bounds__(kThreads) void attend_join_few_kernel(const Args a, int64_t n_rows) {
+  constexpr int kAhead = 8;
+  __shared__ float2 part[kWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
+  const int64_t at = (int64_t)blockIdx.x * (kWaves / W) + wave / W, row = min(at, n_rows - 1);
+  const float* const P = a.partials + row * a.pieces * kPartial;
+  auto state = [&](int i) { return P + (int64_t)min(i, a.pieces - 1) * kPartial; };
+  float m = state(lane)[0], l = state(lane)[1];
+  const int count = __float_as_int(P[2]);
+  float2 x[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) x[j] = *reinterpret_cast<const float2*>(state(w + j * W) + 4 + 2 * lane);
+  const int t = (int)(row / (a.m.Hkv * a.G));
+  const bool mine = at < n_rows && t >= max(a.m.start[0], 0) && t < min(a.m.start[a.m.B], a.m.T);
+  if (W == 1 && !mine) return;
+  const int pieces = __builtin_amdgcn_readfirstlane(min(max(count, 1), a.pieces));
+  float mx = -INFINITY, sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
+  for (int i0 = 0; i0 < pieces; i0 += 64) {
+    if (i0 > 0) {
+      m = state(i0 + lane)[0];
+      l = state(i0 + lane)[1];
+    }
+    if (i0 + lane >= pieces) {
+      m = -INFINITY;
+      l = 0.0f;
+    }
+    float top = fmaxf(mx, m);
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+    const float f = weight_of(m, l, top), g = weight_of(mx, sum, top);
+    float add = l * f;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) add += __shfl_xor(add, i);
+    sum = sum * g + add;
+    x0 *= g;
+    x1 *= g;
+    mx = top;
+    const int n = min(64, pieces - i0);
+    for (int i = w; i < n; i += kAhead * W) {
+      if (i0 > 0 || i > w) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) x[j] = *reinterpret_cast<const float2*>(state(i0 + i + j * W) + 4 + 2 * lane);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j * W < n) {
+          const float k = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i + j * W));
+          x0 = __builtin_fmaf(k, x[j].x, x0);
+          x1 = __builtin_fmaf(k, x[j].y, x1);
+        }
+    }
+  }
+  if constexpr (W > 1) {
+    part[wave][lane] = make_float2(x0, x1);
+    __syncthreads();
+    if (!mine || w != 0) return;
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+      x0 += part[wave + i][lane].x;
+      x1 += part[wave + i][lane].y;
+    }
+  }
+  x0 = sum == 0.0f ? 0.0f : x0 / sum;
+  x1 = sum == 0.0f ? 0.0f : x1 / sum;
+  static_cast<uint32_t*>(a.out)[at * (kD / 2) + lane] = dev::pack_bf16(x0, x1);
+}
+
+constexpr int kFewJoin = 1024; // rows up to which a workgroup joins one of them (1536 rows of 64 sequences: 58 us so, 54 with a wavefront each)
 constexpr int kFewRows = 64;   // rows of the problem up to which pages of 4 bits are attended to by attend_few_kernel
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
@@ -1597,7 +1689,14 @@ hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStr
   if (e != hipSuccess) return e;
   if (a.partials) {
     const int64_t rows = (int64_t)s.T * s.Hq;
-    if (c.pieces > 8)  // a workgroup per row
+    if (c.few) {
+      if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) {
+        if (c.pieces > 8 && rows <= kFewJoin)
+          hipLaunchKernelGGL(attend_join_few_kernel<kWaves>, dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);
+        else
+          hipLaunchKernelGGL(attend_join_few_kernel<1>, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, rows);
+      }
+    } else if (c.pieces > 8)  // a workgroup per row
       hipLaunchKernelGGL((attend_join_kernel<BF16, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);
     else
       hipLaunchKernelGGL((attend_join_kernel<BF16, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0,
