@@ -13,13 +13,15 @@
 // rescaled, only when a score exceeds it by more than kLag powers of two (or, in the tiles' steps, when 16 weights exceed
 // kHeavy); until then it is one of an earlier block, which is exact up to the rounding that the weights have anyway.
 //
-// Three shapes of workgroup, all of four wavefronts:
+// Four shapes of workgroup, all of four wavefronts:
 //   tile  the wavefronts take 32 rows of the problem each and share the positions, 64 at a time (32
 //         in fp32) through two buffers in LDS: K and V are read once for 128 rows
 //   pair  at most 64 rows (bf16): two wavefronts take 32 rows each at one half of every block of 64
 //         positions, the other two the same rows at the other half
 //   thin  at most 32 rows: each wavefront takes every fourth block of 32 positions through an LDS
 //         area of its own, without a barrier
+//   few   pages of 4 bits and bf16, at most 64 rows: as thin, with tiles of 16 rows and blocks of 64
+//         positions, and K from its load into the product, not through LDS
 // The states of wavefronts that have the same rows, and of the pieces that a long context is cut into, are joined at the
 // end.  Rows of the pool's own type go straight to LDS (thin: through registers), codes are decoded on the way into
 // it, exactly: a code times its scale is a bf16 number.
@@ -1208,6 +1210,12 @@ __device__ __forceinline__ int few_chunk(int row, int c) {
 // which lies in one page.  K does not touch LDS; V passes through 16 KB of it.  Two sets of rows share the
 // decoded tiles; both are always worked on (with code of its own for units that have one set of rows only, 180 bytes of registers spilled
 // and the whole took 1.6 to 2 times as long), and the maximum is looked at for both together.
+// One set: bound by memory where there is enough of it: one token of 16 sequences of 8K to 128K, 1.10 GB, 202 us and 5 for the
+// join, 5.4 TB/s (as thin workgroups 265); vector instructions are busy 37 % of the cycles, matrix cores 13 %, no LDS bank
+// conflict.  Blocks two ahead changed nothing; three wavefronts a SIMD do not get the registers without spilling (340 us).  One token at
+// 4K: 6.7 us and 2.6, a chain of loads that wait for each other.  Two sets: bound by the latency of what a block does one after
+// the other, two wavefronts a SIMD covering it; 28 rows of 8 sequences of 32K, 285 MB, 76 to 82 us (thin 128); 1 to 5
+// tokens of 8 sequences of 7K to 64K, 7 heads a group, 99 MB, 40 us and 4 (pairs 48 and 6).  Three sets spill 200 bytes.
 template <int NS>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
   constexpr int M = 16 * NS, BN = 64, kTile = BN * kRowB<true>, kStep = kWaves * BN;
@@ -1520,7 +1528,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 
 // The same for attend_few_kernel's states: the number of a row's pieces stands with its first one, so that a row asks for
 // everything at once, its first states before it knows how many there are, and nothing depends on the number of sequences (a
-// token of 256 sequences, 8192 rows: 101 us in attend_join_kernel, where every row looks through their lengths).  W wavefronts a row:
+// token of 256 sequences, 8192 rows: 101 us in attend_join_kernel, where every row looks through their lengths; the whole call 281 us with
+// that and 198 with this).  2.5 us for a token at 4K, 16 pieces.  W wavefronts a row:
 // all of them weigh all pieces, each adds up every W-th.
 template <int W>
 __global__ __launch_bounds__(kThreads) void attend_join_few_kernel(const Args a, int64_t n_rows) {
@@ -1594,8 +1603,9 @@ constexpr int kFewJoin = 1024; // rows up to which a workgroup joins one of them
 constexpr int kFewRows = 64;   // rows of the problem up to which pages of 4 bits are attended to by attend_few_kernel
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
-// How a call is cut up.  At most 32 rows a sequence and KV head go the thin way, and all calls with pages of less than 16
-// positions, whose rows have a place each (2048 tokens at 32K, bf16: 2360 us, and 1050 with pages of 16 and more; 12 tokens 38 and
+// How a call is cut up.  Pages of 4 bits in bf16 go the few way up to 64 rows: 4 rows 265 us as thin workgroups and 209 so, 28 rows
+// 128 and 82, 32 rows 76 and 52, 35 rows in pairs 73 and 75, 1 to 35 rows 56 and 48, 63 rows 34.6 and 34.1.  Else at most 32 rows a
+// sequence and KV head go the thin way, and all calls with pages of less than 16 positions, whose rows have a place each (2048 tokens at 32K, bf16: 2360 us, and 1050 with pages of 16 and more; 12 tokens 38 and
 // 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
 // more in tiles.
 struct Cut {
@@ -1626,7 +1636,8 @@ Cut cut(const lrqk_pages_shape& s) {
   if (most <= 128 && s.B <= 4096 && (c.rows > 32 || f32 || c.few)) {
     // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
     // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 64 / 72 / 79; 12 tokens of 2 sequences of 32K
-    // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234.  States of 64 MiB at most.
+    // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234; few, one token of 4 sequences of 16K 24 / 29 / -, 16 rows of
+    // 8 of 32K 64 / 75 / - (eight times as many, as thin workgroups have: 113).  States of 64 MiB at most.
     c.want = std::max((held + s.Hkv - 1) / s.Hkv, 2 * tiles);
     c.pieces = (int)std::max(few, std::min<int64_t>({c.want, least, std::max<int64_t>((1ll << 26) / state, 1)}));
     c.units = c.want;

@@ -169,6 +169,8 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
   if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)s.all_x;
 }
 
+// 8.5 us for one sequence of one token, 11.6 for 256 (4.7 for a launch that finds nothing to do): a round trip to memory each for the
+// lengths, the entries given back, their references, the pool's, the table and its entries for the slots, and ten barriers.
 template <bool LDS>
 __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   __shared__ int32_t lds[LDS ? 4 * (kSeqs + 1) : 1];
