@@ -156,7 +156,9 @@ template <int M>
 __device__ __forceinline__ bool find_from(const Args& a, int unit, Problem& p, Seq q, Cursor& from) {
   const int lane = threadIdx.x & 63;
   int before = from.before;
-  for (int i0 = from.i0;;) {
+  const int first = from.i0;
+  for (int i0 = first; i0 < a.m.B; i0 += 64) {
+    if (i0 > first) q = lane_sequence(a, i0);
     const int tiles = (q.n * a.G + M - 1) / M, pieces = max(1, (min(q.len, a.m.l_max) + p.step - 1) / p.step);
     const int units = i0 + lane < a.m.B ? tiles * pieces : 0;
     const int upto = before + (int)dev::wave_inclusive_scan((uint32_t)units);
@@ -179,10 +181,8 @@ __device__ __forceinline__ bool find_from(const Args& a, int unit, Problem& p, S
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
-    i0 += 64;
-    if (i0 >= a.m.B) return false;
-    q = lane_sequence(a, i0);
   }
+  return false;
 }
 template <int M, bool EVEN>
 __device__ __forceinline__ bool find_unit(const Args& a, int unit, Problem& p) {
