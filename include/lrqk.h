@@ -530,6 +530,8 @@ int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pages, int3
  * output, whatever its rows hold.  An infinite element of V under a weight of 0 (a score of -infinity, or one
  * that far below the others) makes NaN or that infinity.  Products of bf16 operands are exact, sums fp32; with bf16 q the
  * weights are rounded to bf16 before they meet V and before they are summed.
+ * (fp32 q over 4-bit pages of 16 positions and more: q and the weights are taken as three bf16 terms each that add up to
+ * them exactly, but for terms below 2^-126.)
  *   q    device kv_dtype [T,Hq,d]
  *   out  device kv_dtype [T,Hq,d]  written
  *   workspace  device, >= lrqk_pages_workspace_bytes(shape), 256-byte aligned

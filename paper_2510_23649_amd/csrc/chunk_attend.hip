@@ -20,8 +20,9 @@
 //         positions, the other two the same rows at the other half
 //   thin  at most 32 rows: each wavefront takes every fourth block of 32 positions through an LDS
 //         area of its own, without a barrier
-//   few   pages of 4 bits and bf16, at most 64 rows: as thin, with tiles of 16 rows and blocks of 64
-//         positions, and K from its load into the product, not through LDS
+//   few   pages of 4 bits, at most 64 rows in bf16 and any number in fp32: as thin, with tiles of 16
+//         rows and blocks of 64 positions, and K from its load into the product, not through LDS; in
+//         fp32 q and the weights as three bf16 terms each
 // The states of wavefronts that have the same rows, and of the pieces that a long context is cut into, are joined at the
 // end.  Rows of the pool's own type go straight to LDS (thin: through registers), codes are decoded on the way into
 // it, exactly: a code times its scale is a bf16 number.
@@ -1109,31 +1110,70 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attend_thin_kernel(con
 // Lane l: row l % 16 of a set; the 16 positions of a tile of S^T are 4 (l / 16) + v, v the register; elements of O^T likewise.
 // A row of K goes straight from its load into the product: the sum over elements may run in any order, so that the lane
 // that holds 32 codes of a row, one block with one scale, multiplies them eight at a time with those eight of its q.
+// In fp32, K and V are exact in bf16 all the same, and q and the weights are sums of three bf16 numbers each, exactly: three bf16
+// products in place of one fp32 product, which takes sixteen times as long as one.  (A term below 2^-126 may count for 0.)
+template <bool BF16>
 struct Set16 {
-  uint4 q[4];   // elements 32 (l / 16) + 8 s .. + 7
-  f32x4 o[8];   // elements 16 t ..
+  static constexpr int kTerms = BF16 ? 1 : 3;  // of q, and of a weight
+  uint4 q[kTerms][4];  // elements 32 (l / 16) + 8 s .. + 7
+  f32x4 o[8];          // elements 16 t ..
   float mx, sum;
-  int see;
+  int see;             // positions that the lane's row sees
 
   __device__ __forceinline__ void start(const void* base, int64_t row, bool negate, int lane) {
     const uint32_t flip = negate ? 0x80008000u : 0u;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      uint4 x = static_cast<const uint4*>(base)[row * 16 + 4 * (lane >> 4) + s];
-      x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
-      q[s] = x;
+      const int64_t chunk = row * 16 + 4 * (lane >> 4) + s;  // eight elements
+      if constexpr (BF16) {
+        uint4 x = static_cast<const uint4*>(base)[chunk];
+        x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+        q[0][s] = x;
+      } else {
+        const float4 x = static_cast<const float4*>(base)[2 * chunk], y = static_cast<const float4*>(base)[2 * chunk + 1];
+        uint32_t t[4][3];
+        terms(x.x, x.y, t[0]);
+        terms(x.z, x.w, t[1]);
+        terms(y.x, y.y, t[2]);
+        terms(y.z, y.w, t[3]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) q[i][s] = make_uint4(t[0][i] ^ flip, t[1][i] ^ flip, t[2][i] ^ flip, t[3][i] ^ flip);
+      }
     }
 #pragma unroll
     for (int t = 0; t < 8; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     mx = -INFINITY;
     sum = 0.0f;
   }
-  // scores of 16 positions: a tile of K, row l % 16, block l / 16, eight elements each
-  __device__ __forceinline__ f32x4 scores(const uint4 (&tile)[4]) const {
+  // Two fp32 numbers as three pairs of bf16 numbers that add up to them, exactly: the upper eight bits of their significands, the next
+  // eight, the rest.  One that is not finite is its own first term, without others.
+  static __device__ __forceinline__ void terms(float x, float y, uint32_t (&t)[3]) {
+    const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
+    t[0] = __builtin_amdgcn_perm(v, u, 0x07060302u);  // the upper halves
+    float dx = x - __uint_as_float(u & 0xffff0000u), dy = y - __uint_as_float(v & 0xffff0000u);
+    if ((u & 0x7f800000u) == 0x7f800000u) dx = 0.0f;
+    if ((v & 0x7f800000u) == 0x7f800000u) dy = 0.0f;
+    more_terms(dx, dy, t);
+    if (((u & 0x7f800000u) == 0x7f800000u) && (u & 0x7fffffu)) t[0] |= 0x00007fffu;  // (a NaN stays one without its lower half)
+    if (((v & 0x7f800000u) == 0x7f800000u) && (v & 0x7fffffu)) t[0] |= 0x7fff0000u;
+  }
+  static __device__ __forceinline__ void more_terms(float dx, float dy, uint32_t (&t)[3]) {
+    const uint32_t u = __float_as_uint(dx), v = __float_as_uint(dy);
+    t[1] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+    dx -= __uint_as_float(u & 0xffff0000u);
+    dy -= __uint_as_float(v & 0xffff0000u);
+    t[2] = __builtin_amdgcn_perm(__float_as_uint(dy), __float_as_uint(dx), 0x07060302u);
+  }
+  // scores of 16 positions: a tile of K, row l % 16, block l / 16, eight elements each; `low`: what q's terms after the first
+  // meet, the same without elements that are not finite (an infinity times a term of 0 would be NaN)
+  __device__ __forceinline__ f32x4 scores(const uint4 (&tile)[4], const uint4 (&low)[4]) const {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, tile[k]), __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
+    for (int i = kTerms - 1; i >= 0; --i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, i > 0 ? low[k] : tile[k]), __builtin_bit_cast(bf16x8, q[i][k]), s,
+                                                    0, 0, 0);
     return s;
   }
   // scores of the 16 positions from p0 that the row does not see, or that are not there, become -infinity
@@ -1170,10 +1210,13 @@ struct Set16 {
       for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
     return over_lanes(top) * c;
   }
-  // Weights of 64 positions (see Rows::weigh and weigh_any) as the second product's operands, 32 each.  far: some row's maximum is
+  // Weights of 64 positions (see Rows::weigh and weigh_any) as the second product's operands, 32 each.  FAR: some row's maximum is
   // beyond kFar.
+  struct Weights {
+    uint4 of[2][kTerms];
+  };
   template <bool FAR>
-  __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, uint4 (&x)[2]) {
+  __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, Weights& x) {
     const float base = mx == -INFINITY ? 0.0f : mx;
     const bool rounded = FAR && fabsf(mx) >= kFar;
     const auto weight = [&](float y) {
@@ -1189,17 +1232,29 @@ struct Set16 {
     float add[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      uint32_t w[4];
+      uint32_t w[4][3];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        w[e] = dev::pack_bf16(weight(s[2 * i + e / 2][2 * e % 4]), weight(s[2 * i + e / 2][2 * e % 4 + 1]));
-        add[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e]), one, add[i], false);
+        const float u = weight(s[2 * i + e / 2][2 * e % 4]), v = weight(s[2 * i + e / 2][2 * e % 4 + 1]);
+        if constexpr (BF16) {
+          w[e][0] = dev::pack_bf16(u, v);
+          add[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(dev::bf16x2, w[e][0]), one, add[i], false);
+        } else {  // (a weight that is not finite makes its row NaN through any of them)
+          w[e][0] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302u);
+          more_terms(u - __uint_as_float(__float_as_uint(u) & 0xffff0000u), v - __uint_as_float(__float_as_uint(v) & 0xffff0000u), w[e]);
+          add[i] += u + v;
+        }
       }
-      x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+      for (int n = 0; n < kTerms; ++n) x.of[i][n] = make_uint4(w[0][n], w[1][n], w[2][n], w[3][n]);
     }
     sum += add[0] + add[1];
   }
 };
+__device__ __forceinline__ uint4 cleared_chunk(uint4 x) {
+  return make_uint4(clear<true>(x.x), clear<true>(x.y), clear<true>(x.z), clear<true>(x.w));
+}
+constexpr uint32_t kOddScale = 253;  // scale byte of e2m1 from which an element can be an infinity, or NaN
 // Where LDS holds chunk c of a row of V: eight rows' same chunk (as they are stored) lies in eight places mod 8, eight rows' two
 // chunks (as they are read) in sixteen.
 __device__ __forceinline__ int few_chunk(int row, int c) {
@@ -1216,8 +1271,12 @@ __device__ __forceinline__ int few_chunk(int row, int c) {
 // 4K: 6.7 us and 2.6, a chain of loads that wait for each other.  Two sets: bound by the latency of what a block does one after
 // the other, two wavefronts a SIMD covering it; 28 rows of 8 sequences of 32K, 285 MB, 76 to 82 us (thin 128); 1 to 5
 // tokens of 8 sequences of 7K to 64K, 7 heads a group, 99 MB, 40 us and 4 (pairs 48 and 6).  Three sets spill 200 bytes.
-template <int NS>
+// fp32, one set, bound by the products and the vector instructions about them: with the joins, one token of 16 sequences of up to 128K
+// 293 us (on the fp32 matrix cores, 32 rows a tile, 2486), the drafts 58 (399), 1001 tokens at 5003 and 744 at 1315 283 (676), 2048 tokens
+// at 32K 3.3 ms, 322 TFLOP/s (8.3).
+template <int NS, bool BF16>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
+  using Set = Set16<BF16>;
   constexpr int M = 16 * NS, BN = 64, kTile = BN * kRowB<true>, kStep = kWaves * BN;
   __shared__ __align__(16) char lds[kWaves * kTile];  // a wavefront's rows of V; then the states
   __shared__ float wm[kWaves * M], ws[kWaves * M];
@@ -1225,6 +1284,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
   const int kvh = blockIdx.x % a.m.Hkv;
   const uint4* const K = static_cast<const uint4*>(a.K);
   const uint4* const V = static_cast<const uint4*>(a.V);
+  __shared__ int odd_from[2];  // fp32: first block that something was left out of, in this unit and the next
+  int turn = 0;
+  if (!BF16) {
+    if (threadIdx.x < 2) odd_from[threadIdx.x] = INT32_MAX;
+    __syncthreads();
+  }
   Problem p;
   Cursor cursor{0, 0};
   Seq first = lane_sequence(a, 0);
@@ -1237,7 +1302,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
     const int least = sees(a, p, p.r0), most = sees(a, p, p.r0 + rows - 1);
     const int from = p.piece * p.step, end = min(most, from + p.step);
     if (from >= end && p.piece > 0) continue;  // (piece 0 writes the rows that see nothing)
-    Set16 r[NS];
+    Set r[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       const int real = min(p.r0 + 16 * n + (lane & 15), p.rows - 1);
@@ -1284,7 +1349,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
       bool far = false;
       for (int p0 = mine; p0 < end; p0 += kStep) {
         const bool part = p0 + BN > least, more = p0 + kStep < end;
+        // fp32: what is not finite is left out wherever it is, since it would meet weights' terms that are 0
+        const bool leave_out = part || (!BF16 && __any(max(max(vs[0], vs[1]), max(vs[2], vs[3])) >= kOddScale));
         const bool whole = !part && (there[0] & there[1] & there[2] & there[3]) == 0xffffu;
+        bool left = false;
         uint32_t now[4];
         // V into LDS, all 64 positions, long before it is read
         __builtin_amdgcn_wave_barrier();  // the wavefront's LDS operations execute in order
@@ -1296,16 +1364,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             uint4 y = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
-            if (!whole) {
+            if (!whole || leave_out) {
               if (!((now[i] >> (lane & 15)) & 1)) y = make_uint4(0, 0, 0, 0);
-              if (part) {
-                cleared |= odd<true>(y.x) || odd<true>(y.y) || odd<true>(y.z) || odd<true>(y.w);
-                y = make_uint4(clear<true>(y.x), clear<true>(y.y), clear<true>(y.z), clear<true>(y.w));
+              if (leave_out) {
+                left |= odd<true>(y.x) || odd<true>(y.y) || odd<true>(y.z) || odd<true>(y.w);
+                y = cleared_chunk(y);
               }
             }
             *reinterpret_cast<uint4*>(vt + few_chunk(16 * i + (lane & 15), 4 * (lane >> 4) + j)) = y;
           }
         }
+        cleared |= left;
+        if (!BF16 && left) atomicMin(&odd_from[turn], p0);
         if (more) {
           find(p0 + kStep);
           fetch(V, a.V_scale, v, vs);
@@ -1318,8 +1388,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
           uint4 tile[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) tile[j] = decode8_bf16<LRQK_PAGE_E2M1>(word[j], f);
+          if (!BF16 && __builtin_expect(__any(ks[i] >= kOddScale), 0)) {
+            uint4 low[4];
 #pragma unroll
-          for (int n = 0; n < NS; ++n) s[n][i] = r[n].scores(tile);
+            for (int j = 0; j < 4; ++j) low[j] = cleared_chunk(tile[j]);
+            s[0][i] = r[0].scores(tile, low);
+          } else {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) s[n][i] = r[n].scores(tile, tile);
+          }
         }
         if (more) {
           fetch(K, a.K_scale, k, ks);
@@ -1337,7 +1414,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
         }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          top[n] = Set16::largest(s[n], c);
+          top[n] = Set::largest(s[n], c);
           raise |= top[n] > r[n].mx + kLag;
         }
         if (__any(raise)) {
@@ -1349,7 +1426,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
           }
           far = __any(beyond);
         }
-        uint4 x[NS][2];
+        typename Set::Weights x[NS];
         if (__builtin_expect(far, 0)) {
 #pragma unroll
           for (int n = 0; n < NS; ++n) r[n].template weigh<true>(s[n], c, x[n]);
@@ -1371,7 +1448,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
             const bf16x8 z = __builtin_bit_cast(bf16x8, __builtin_shufflevector(y[0], y[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int n = 0; n < NS; ++n)
-              r[n].o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z, __builtin_bit_cast(bf16x8, x[n][half]), r[n].o[t], 0, 0, 0);
+#pragma unroll
+              for (int i = Set::kTerms - 1; i >= 0; --i)
+                r[n].o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z, __builtin_bit_cast(bf16x8, x[n].of[half][i]), r[n].o[t], 0, 0, 0);
           }
         }
       }
@@ -1384,21 +1463,23 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
 #pragma unroll
       for (int t = 0; t < 8; ++t)
         *reinterpret_cast<f32x4*>(acc + (size_t)to * kD + 4 * ((4 * t + (lane >> 4)) ^ i)) = r[n].o[t];
-      const float sum = Set16::sum_lanes(r[n].sum);
+      const float sum = Set::sum_lanes(r[n].sum);
       if (lane < 16) {
         wm[to] = r[n].mx;
         ws[to] = sum;
       }
     }
     __syncthreads();
-    join_states<true>(a, p, kvh, rows, kWaves, M, acc, wm, ws);
+    join_states<BF16>(a, p, kvh, rows, kWaves, M, acc, wm, ws);
     if (a.partials && p.piece == 0 && (int)threadIdx.x < rows) {  // what attend_join_few_kernel goes by
       const int row = p.r0 + threadIdx.x;
       const int64_t at = (int64_t)(p.s.first + row / a.G) * (a.m.Hkv * a.G) + kvh * a.G + row % a.G;
       a.partials[at * a.pieces * kPartial + 2] = __int_as_float(max(1, (most + p.step - 1) / p.step));
     }
+    if (!BF16 && threadIdx.x == 0) odd_from[turn ^ 1] = INT32_MAX;  // (nobody looks at that one before the next unit)
     if (__syncthreads_or(cleared))
-      add_left_out<true, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, kWaves, M);
+      add_left_out<BF16, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, BF16 ? max(from, least - least % BN) : odd_from[turn], end, ws, kWaves, M);
+    turn ^= 1;
   }
 }
 
@@ -1531,7 +1612,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 // token of 256 sequences, 8192 rows: 101 us in attend_join_kernel, where every row looks through their lengths; the whole call 281 us with
 // that and 198 with this).  2.5 us for a token at 4K, 16 pieces.  W wavefronts a row:
 // all of them weigh all pieces, each adds up every W-th.
-template <int W>
+template <bool BF16, int W>
 __global__ __launch_bounds__(kThreads) void attend_join_few_kernel(const Args a, int64_t n_rows) {
   constexpr int kAhead = 8;
   __shared__ float2 part[kWaves][64];
@@ -1596,7 +1677,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_few_kernel(const Args a,
   }
   x0 = sum == 0.0f ? 0.0f : x0 / sum;
   x1 = sum == 0.0f ? 0.0f : x1 / sum;
-  static_cast<uint32_t*>(a.out)[at * (kD / 2) + lane] = dev::pack_bf16(x0, x1);
+  if constexpr (BF16) static_cast<uint32_t*>(a.out)[at * (kD / 2) + lane] = dev::pack_bf16(x0, x1);
+  else static_cast<float2*>(a.out)[at * (kD / 2) + lane] = make_float2(x0, x1);
 }
 
 constexpr int kFewJoin = 1024; // rows up to which a workgroup joins one of them (1536 rows of 64 sequences: 58 us so, 54 with a wavefront each)
@@ -1604,7 +1686,8 @@ constexpr int kFewRows = 64;   // rows of the problem up to which pages of 4 bit
 constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 
 // How a call is cut up.  Pages of 4 bits in bf16 go the few way up to 64 rows: 4 rows 265 us as thin workgroups and 209 so, 28 rows
-// 128 and 82, 32 rows 76 and 52, 35 rows in pairs 73 and 75, 1 to 35 rows 56 and 48, 63 rows 34.6 and 34.1.  Else at most 32 rows a
+// 128 and 82, 32 rows 76 and 52, 35 rows in pairs 73 and 75, 1 to 35 rows 56 and 48, 63 rows 34.6 and 34.1; in fp32 all calls (see
+// attend_few_kernel).  Else at most 32 rows a
 // sequence and KV head go the thin way, and all calls with pages of less than 16 positions, whose rows have a place each (2048 tokens at 32K, bf16: 2360 us, and 1050 with pages of 16 and more; 12 tokens 38 and
 // 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
 // more in tiles.
@@ -1618,8 +1701,8 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t most = (int64_t)s.n_max * G;
   const bool f32 = s.kv_dtype == LRQK_KV_F32;
   Cut c;
-  c.few = s.page_dtype == LRQK_PAGE_E2M1 && !f32 && s.page >= 16 && most <= kFewRows;
-  c.rows = c.few ? (most <= 16 ? 16 : 32) : most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
+  c.few = s.page_dtype == LRQK_PAGE_E2M1 && s.page >= 16 && (f32 || most <= kFewRows);
+  c.rows = c.few ? (most <= 16 || f32 ? 16 : 32) : most <= 32 || s.page < 16 ? 32 : most <= 64 && !f32 ? 64 : 128;
   const int full = (int)(((int64_t)s.T * G + c.rows - 1) / c.rows), tiles = full + s.B;  // sum_b ceil(n_b G / rows) is no more
   const int64_t units = (int64_t)std::max(s.B, full) * s.Hkv;
   // workgroups that the chip holds at a time: two on each of 256 compute units where registers allow it
@@ -1689,9 +1772,9 @@ hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStr
   hipError_t e = hipSuccess;
   if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
   else if (c.few) {
-    if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) {
-      if (c.rows == 16) hipLaunchKernelGGL(attend_few_kernel<1>, grid, dim3(kThreads), 0, st, a);
-      else hipLaunchKernelGGL(attend_few_kernel<2>, grid, dim3(kThreads), 0, st, a);
+    if constexpr (PAGE == LRQK_PAGE_E2M1) {
+      if (c.rows == 16) hipLaunchKernelGGL((attend_few_kernel<1, BF16>), grid, dim3(kThreads), 0, st, a);
+      else if constexpr (BF16) hipLaunchKernelGGL((attend_few_kernel<2, BF16>), grid, dim3(kThreads), 0, st, a);
     }
   } else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
   else if (c.rows == 64) {
@@ -1701,11 +1784,11 @@ hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStr
   if (a.partials) {
     const int64_t rows = (int64_t)s.T * s.Hq;
     if (c.few) {
-      if constexpr (BF16 && PAGE == LRQK_PAGE_E2M1) {
+      if constexpr (PAGE == LRQK_PAGE_E2M1) {
         if (c.pieces > 8 && rows <= kFewJoin)
-          hipLaunchKernelGGL(attend_join_few_kernel<kWaves>, dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);
+          hipLaunchKernelGGL((attend_join_few_kernel<BF16, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);
         else
-          hipLaunchKernelGGL(attend_join_few_kernel<1>, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, rows);
+          hipLaunchKernelGGL((attend_join_few_kernel<BF16, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, rows);
       }
     } else if (c.pieces > 8)  // a workgroup per row
       hipLaunchKernelGGL((attend_join_kernel<BF16, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, a, rows);

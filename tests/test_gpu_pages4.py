@@ -251,6 +251,51 @@ def test_huge_scores_all_alike(way, kv):
         assert (np.abs(got - y) <= tol).all(), (code, byte, np.abs(got - y).max())
 
 
+@pytest.mark.parametrize("kv", KV)
+@pytest.mark.parametrize("way", WAYS)
+def test_queries_of_every_size(way, kv):
+    """Blocks of q of very different size, those of K the other way round: every block counts for the score, in all its bits."""
+    n, ln = WAYS[way]
+    c = make([(n, ln), (1, 33)], 1, 3, 16, kv, seed=67, qs=1.0)
+    for b, e in enumerate((-60, -20, 25, 70)):
+        c.q[..., 32 * b:32 * b + 32] *= 2.0 ** e
+        c.sc["K"][..., b] = (c.sc["K"][..., b].int() - e).to(torch.uint8)
+    c.poison(np.ones((c.n_pages, c.page), bool) & ~np.isin(np.arange(c.n_pages), c.table)[:, None])
+    c.to_device()
+    c.check_attend(c.attend())
+
+
+@pytest.mark.parametrize("kv", KV)
+@pytest.mark.parametrize("way", WAYS)
+def test_queries_that_are_no_numbers(way, kv):
+    """NaN and infinities in q reach their own head and token alone; scores of -infinity alone give zeros."""
+    n, ln = WAYS[way]
+    c = make([(n, ln), (1, 33)], 1, 3, 16, kv, seed=68)
+    low_nan = torch.tensor([0x7F800001], dtype=torch.int32).view(torch.float32)[0].to(P.TYPE[kv])   # (fp32: its upper half is an infinity)
+    bad = [(0, 0, float("nan")), (n - 1, 1, low_nan if kv == "f32" else float("nan")), (n, 2, float("inf")), (n, 0, -float("inf")), (0, 2, 3.0e38)]
+    clean = c.q.clone()
+    for t, h, v in bad:
+        c.q[t, h, 7] = v
+    for p in range(int(c.len[1])):                           # sequence 1: -1 in K's element 7 under both infinities
+        pg, o = c.where(1, p)
+        set_code(c, "K", pg, 0, o, 7, 10)
+        c.sc["K"][pg, 0, o, 0] = 127
+    c.to_device()
+    got = c.attend()
+    assert torch.isnan(got[0, 0]).all() and torch.isnan(got[n - 1, 1]).all()
+    assert (got[n, 2] == 0).all(), "infinity times -1: scores of -infinity alone"
+    assert torch.isnan(got[n, 0]).all(), "scores of +infinity"
+    # (3.0e38 times a K of 1.5 and more is beyond fp32: that token and head may be anything, the others not)
+    c.q = clean
+    want = c.attend()
+    same = torch.ones_like(got, dtype=torch.bool)
+    for t, h, _ in bad:
+        same[t, h] = False
+    # the others within the bound: rows that share a wavefront have their maxima raised together, so that their roundings may differ
+    c.check_attend(want)
+    c.check_attend(torch.where(same, got, want))
+
+
 def test_n_max_only_chooses_the_kernel():
     for seqs in ([(1, 700), (1, 90)], [(4, 300), (1, 900)], [(30, 300), (64, 64)]):
         for n_max in (1, 2, 4, 8, 16, 40, 1000):
