@@ -19,8 +19,10 @@ constexpr int kTile = kThreads * 16;  // pages looked at together: a wavefront t
 // Rows whose maps the one workgroup makes (256 sequences, 4096 rows: 13.0 us, and 15.1 with a launch of their own; 8448: 16.3 and 15.9).
 constexpr int kRowsHere = 6144;
 constexpr int kSmall = 2;  // pages of a sequence that its own thread gives back or takes
-// Pages whose counts the one workgroup looks through: 64K of them take it 4.5 us, and two launches 5 however many there are.
-constexpr int kPagesHere = 4 * kTile;
+// Pages that the one workgroup looks through itself, as far as it has to: 4.5 us for 64K of them.  Two launches before it that give pages
+// back and count take 6, however many there are.  256 sequences of one token, 80K to 144K pages: 11.9 us where free ones lie in front and
+// 17.8 to 21.8 where only the last ones are free, 17.7 with counts; 1M pages at their end 17 with counts and 96 without.
+constexpr int kPagesHere = 9 * kTile;
 
 struct Args {
   int32_t *refs, *table, *kv_len, *start, *status, *seq, *pos, *slot;
