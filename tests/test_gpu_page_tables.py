@@ -171,7 +171,7 @@ def test_many_sequences(B):
     consistent(t)
 
 
-@pytest.mark.parametrize("n_pages", [1, 3, 1023, 4097, 16384, 16385, 50001, 200003])
+@pytest.mark.parametrize("n_pages", [1, 3, 1023, 4097, 16384, 16385, 50001, 81920, 81921, 140001, 147456, 147457, 200003])
 def test_pools(n_pages):
     """Pools up to many times of what is looked at together: free pages only at their end, all over, or none."""
     rng = np.random.default_rng(n_pages)
@@ -184,7 +184,23 @@ def test_pools(n_pages):
         t.step([0, 0, 0, 0, 0], [700, 4, 700, 4, 4])
 
 
-@pytest.mark.parametrize("T", [1, 8191, 8192, 8193, 40000])
+@pytest.mark.parametrize("B", [1500, 2500])
+def test_many_sequences_and_a_large_pool(B):
+    rng = np.random.default_rng(B)
+    t = Tables(B, 2, 170000, 6 * B, 300, 900)
+    t.refs[:] = rng.random(170000) < 0.9
+    t.refs[:120000] = 1
+    t.put()
+    n = rng.integers(0, 6, B)
+    n[::200] = 300
+    t.step(None, n)
+    for i in range(3):
+        keep = np.maximum(t.kv_len - rng.integers(0, 5, B), 0)
+        keep[rng.random(B) < 0.05] = 0
+        t.step(keep, rng.integers(0, 7, B), f"step {i}", twice=True)
+
+
+@pytest.mark.parametrize("T", [1, 6144, 6145, 8191, 8192, 8193, 40000])
 def test_rows(T):
     """Maps of few rows and of many, rows of no sequence behind them, one map alone or none."""
     for maps in (("seq", "pos", "slot"), ("pos",), ("slot",), ("seq",), ()):
