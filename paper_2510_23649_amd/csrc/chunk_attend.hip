@@ -113,7 +113,7 @@ __device__ __forceinline__ int piece_of(const Args& a, Seq s) {
   const int lane = threadIdx.x & 63;
   int longest = 0, p;
   if (EVEN && a.want > 0) {
-    uint32_t x = 0, t = 0, len, mine;  // lengths in 128 positions; 32 bits hold x: want > 0 only if B <= 4096
+    uint32_t x = 0, t = 0, len, mine;  // lengths in 128 positions; 32 bits hold x: want > 0 only if B <= 4096, or 2048 with 16 rows a tile
     for (int i0 = 0;;) {
       mine = i0 + lane < a.m.B ? (uint32_t)tiles_of(a, s.n) : 0;
       len = mine > 0 ? ((uint32_t)min(s.len, a.m.l_max) + 127) >> 7 : 0;
@@ -1716,7 +1716,7 @@ Cut cut(const lrqk_pages_shape& s) {
   const int64_t least = (s.l_max + c.least - 1) / c.least;  // pieces, with those
   c.prefer = 1;
   c.want = 0;
-  if (most <= 128 && s.B <= 4096 && (c.rows > 32 || f32 || c.few)) {
+  if (most <= 128 && s.B <= (c.rows == 16 ? 2048 : 4096) && (c.rows > 32 || f32 || c.few)) {
     // Workgroups that are bound by more than memory: as many units as the chip holds, one each.  In us with as many / twice /
     // three times as many: 1 to 5 tokens of 8 sequences of 7K to 64K, i8, 64 / 72 / 79; 12 tokens of 2 sequences of 32K
     // 63 / 76 / 86; fp32, one token of 4 sequences of 32K 206 / 218 / 234; few, one token of 4 sequences of 16K 24 / 29 / -, 16 rows of
@@ -1769,7 +1769,8 @@ template <bool BF16, int PAGE>
 hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStream_t st) {
   // as large as the chip, but for the few way with many units: there the next workgroup takes the next one (2048 tokens at 32K in fp32
   // 3.29 ms with 512 workgroups, 3.18 so, prompts of up to 2000 510 and 481 us)
-  const int most = c.few && c.want == 0 ? c.units : std::max(1, kFewGrid / s.Hkv);
+  // (not more than a launch may have)
+  const int most = std::max(1, (c.few && c.want == 0 ? 1 << 20 : kFewGrid) / s.Hkv);
   const dim3 grid((unsigned)(s.Hkv * (c.rows == 128 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
   if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
