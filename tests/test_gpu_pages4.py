@@ -313,6 +313,14 @@ def test_many_and_uneven_sequences():
             c.check_attend(c.attend())
 
 
+@pytest.mark.parametrize("B,kv", [(2048, "f32"), (2049, "f32"), (2049, "bf16"), (4200, "bf16")])
+def test_thousands_of_sequences(B, kv):
+    rng = np.random.default_rng(B)
+    seqs = [(int(rng.integers(0, 3)), int(rng.integers(2, 25))) for _ in range(B - 1)] + [(2, 700)]
+    c = make([seqs[i] for i in rng.permutation(B)], 1, 2, 16, kv, seed=17).to_device()
+    c.check_attend(c.attend())
+
+
 def test_shared_pages():
     for kv in KV:
         c = make([(3, 100), (40, 90), (1, 60)], 2, 4, 16, kv, seed=12)
