@@ -150,6 +150,19 @@ def test_in_place(rot, layout, dt):
         assert torch.equal(v, v0)
 
 
+@pytest.mark.parametrize("dt", [B16, F32])
+def test_many_heads_and_many_tokens(dt):
+    g = torch.Generator().manual_seed(11)
+    for T, Hq, Hkv in ((2, 1024, 1), (3, 1, 1023), (9000, 2, 1)):
+        rope, f, a = rope_of(128, layout=T % 2)
+        pos = torch.randint(0, 100000, (T,), generator=g, dtype=torch.int32).to(DEV)
+        q, k = torch.randn(T, Hq, D, generator=g).to(dt).to(DEV), torch.randn(T, Hkv, D, generator=g).to(dt).to(DEV)
+        qo, ko = torch.full_like(q, MARK), torch.full_like(k, MARK)
+        L.lrqk_rotate(rope, pos, q, qo, k, ko)
+        check(qo, q, pos, f, a, T % 2, False)
+        check(ko, k, pos, f, a, T % 2, False)
+
+
 def test_one_of_both():
     g = torch.Generator().manual_seed(5)
     rope, f, a = rope_of(128)
@@ -284,6 +297,13 @@ def test_positions_that_do_not_exist(maps):
         for kv, pages in (("bf16", "e2m1"), ("f32", "f32")):
             c = Case(seqs, 2, 4, 16, kv, pages, seed=3, l_max=l_max).to_device()
             both(c, rope_of(128)[0], maps)
+
+
+@pytest.mark.parametrize("kv,pages", [("bf16", "e2m1"), ("f32", "f32")])
+def test_many_heads_of_pages(kv, pages):
+    for maps in (False, True):
+        c = Case([(3, 20), (1, 9)], 33, 8, 16, kv, pages, seed=31).to_device()
+        both(c, rope_of(62, layout=0)[0], maps)
 
 
 def test_many_sequences_and_tokens():
