@@ -1732,9 +1732,10 @@ Cut cut(const lrqk_pages_shape& s) {
       c.prefer = (int)std::min<int64_t>(((int64_t)held * (s.B == 1 ? 1 : 8) + units - 1) / units, least);
     } else {
       // many tiles: the fewest rounds of `held` workgroups per piece; a piece more costs some hundredths (700 tokens at 20K,
-      // 176 tiles of 8 heads: 347 us with 3 pieces, which make 528 workgroups, and 274 with 5)
+      // 176 tiles of 8 heads: 347 us with 3 pieces, which make 528 workgroups, and 274 with 5); the few way deals its units out as
+      // workgroups end, and has one piece from four rounds on (2100 tokens at 20K, fp32: 2062 us with two, 2041 with one)
       double best = 0.0;
-      for (int n = 1; n <= 16; ++n) {
+      for (int n = 1; n <= (c.few && units >= 4 * held ? 1 : 16); ++n) {
         const double cost = (double)((units * n + held - 1) / held) / n * (1.0 + 0.04 * (n - 1));
         if (n == 1 || cost < best) {
           c.prefer = n;
