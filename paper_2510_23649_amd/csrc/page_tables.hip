@@ -16,12 +16,12 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kSeqs = 2048;           // sequences whose numbers LDS holds
 constexpr int kTile = kThreads * 16;  // pages looked at together: a wavefront takes 1024 of them, four loads of four a lane
-// Rows whose maps the one workgroup makes (256 sequences, 4096 rows: 13.0 us, and 15.1 with a launch of their own; 8448: 16.3 and 15.9).
+// Rows whose maps the one workgroup makes (256 sequences, 4096 rows: 10.0 us, and 12.0 with a launch of their own; 6144: 12.1 and 12.7; 8448: 14.4 and 13.8).
 constexpr int kRowsHere = 6144;
 constexpr int kSmall = 2;  // pages of a sequence that its own thread gives back or takes
-// Pages that the one workgroup looks through itself, as far as it has to: 4.5 us for 64K of them.  Two launches before it that give pages
-// back and count take 6, however many there are.  256 sequences of one token, 80K to 144K pages: 11.9 us where free ones lie in front and
-// 17.8 to 21.8 where only the last ones are free, 17.7 with counts; 1M pages at their end 17 with counts and 96 without.
+// Pages that the one workgroup looks through itself, as far as it has to: 3.6 us for 64K of them.  Two launches before it that give pages
+// back and count take 5.4, however many there are.  256 sequences of one token, 64K to 144K pages: 9.8 us where free ones lie in front and
+// 15.1 to 18.8 where only the last ones are free, 15.2 to 15.6 with counts; 1M pages at their end 15.4 with counts and 113 without.
 constexpr int kPagesHere = 9 * kTile;
 
 struct Args {
@@ -36,30 +36,39 @@ struct Args {
 __device__ __forceinline__ int pages_of(const Args& a, int len) { return (len + (1 << a.page_log2) - 1) >> a.page_log2; }
 
 // Sums over the workgroup's threads before this one, and of all, of two numbers at a time: a wavefront's sum of numbers up to 2^24
-// fits 32 bits, the workgroup's need not.  One barrier: the totals of one scan are read while the next one writes the others.
+// fits 32 bits; the workgroup's need not and stays at the largest, above all that it is compared with.  Each wavefront reads a total a
+// lane and adds them up along a row of 16.  One barrier, at which nothing waits for memory: the totals of one scan are read while
+// the next one writes the others.  MEM: what threads exchange lies in memory.
 struct Totals {
   uint2 of[2][kWaves];
 };
 struct Sums {
-  uint64_t x, y, all_x, all_y;
+  uint64_t x, y;
+  uint32_t all_x, all_y;
 };
+__device__ __forceinline__ uint32_t sum_row(uint32_t v) {
+  v = __builtin_elementwise_add_sat(v, dev::dpp_zero_fill<0x111, 0xf>(v));  // row_shr:1
+  v = __builtin_elementwise_add_sat(v, dev::dpp_zero_fill<0x112, 0xf>(v));
+  v = __builtin_elementwise_add_sat(v, dev::dpp_zero_fill<0x114, 0xf>(v));
+  return __builtin_elementwise_add_sat(v, dev::dpp_zero_fill<0x118, 0xf>(v));
+}
+template <bool MEM = false>
 __device__ __forceinline__ Sums scan(uint32_t x, uint32_t y, Totals& tot, int& turn) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t ux = dev::wave_inclusive_scan(x), uy = dev::wave_inclusive_scan(y);
   uint2* const of = tot.of[turn];
   turn ^= 1;
   if (lane == 63) of[w] = make_uint2(ux, uy);
-  __syncthreads();
-  Sums s{ux - x, uy - y, 0, 0};
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    const uint2 t = of[i];
-    s.x += i < w ? t.x : 0u;
-    s.y += i < w ? t.y : 0u;
-    s.all_x += t.x;
-    s.all_y += t.y;
+  if constexpr (MEM) {
+    __syncthreads();
+  } else {
+    dev::lds_barrier();
   }
-  return s;
+  const uint2 t = of[lane & 15];
+  const uint32_t tx = sum_row(t.x), ty = sum_row(t.y);
+  const uint32_t bx = w ? __builtin_amdgcn_readlane(tx, w - 1) : 0, by = w ? __builtin_amdgcn_readlane(ty, w - 1) : 0;
+  return Sums{(uint64_t)bx + (ux - x), (uint64_t)by + (uy - y), (uint32_t)__builtin_amdgcn_readlane(tx, 15),
+              (uint32_t)__builtin_amdgcn_readlane(ty, 15)};
 }
 
 // The last of x[0 .. n) (ascending, x[0] <= v) that is not above v.
@@ -171,8 +180,10 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
   if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)s.all_x;
 }
 
-// 8.5 us for one sequence of one token, 11.6 for 256 (4.7 for a launch that finds nothing to do): a round trip to memory each for the
-// lengths, the entries given back, their references, the pool's, the table and its entries for the slots, and ten barriers.
+// 6.7 us for one sequence of one token, 9.7 for 256 (3.8 for a launch that finds nothing to do): a round trip to memory each for the
+// lengths, the entries given back, their references, the pool's, the table and its entries for the slots, and ten barriers.  What
+// most of them share lies in LDS, so that they wait for no store or load; with barriers that do, and all sixteen totals of a scan read by
+// every thread (128 registers and 19 spilled; now 86), 8.5 and 11.6.
 template <bool LDS>
 __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   __shared__ int32_t lds[LDS ? 4 * (kSeqs + 1) : 1];
@@ -216,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
         n_gone = 0;
       }
     }
-    const Sums s = scan((uint32_t)n_gone, 0u, tot, turn);
+    const Sums s = scan<!LDS>((uint32_t)n_gone, 0u, tot, turn);
     if (b < a.B) rank[b] = (int32_t)min(gone + s.x, (uint64_t)INT32_MAX);
     gone += s.all_x;
   }
@@ -253,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
       n = max(n, 0);
       if (need > kSmall) big = 1;
     }
-    const Sums s = scan((uint32_t)need, (uint32_t)n, tot, turn);
+    const Sums s = scan<!LDS>((uint32_t)need, (uint32_t)n, tot, turn);
     if (b < a.B) {
       rank[b] = (int32_t)min(asked + s.x, (uint64_t)INT32_MAX);
       start[b] = n > 0 && rows + s.y + n > (uint64_t)a.T ? LRQK_ADVANCE_ROWS : 0;
@@ -269,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
   uint64_t ahead = 0, in_tile = 0;
   auto count = [&]() __attribute__((always_inline)) {  // what `mask` says
     const uint32_t n = in_wave(mask, before);
-    const Sums s = scan(lane == 0 ? n : 0u, 0u, tot, turn);
+    const Sums s = scan<!LDS>(lane == 0 ? n : 0u, 0u, tot, turn);
     ahead = __builtin_amdgcn_readfirstlane((uint32_t)s.x);  // of lane 0: the wavefronts before
     in_tile = s.all_x;
   };
@@ -278,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
     for (int i0 = 0; i0 < tiles && there < asked; i0 += kThreads) {
       const int n = i0 + (int)threadIdx.x < tiles ? a.counts[i0 + threadIdx.x] : 0;
       if (n > 0) atomicMin(&first_tile, i0 + (int)threadIdx.x);
-      there += scan((uint32_t)n, 0u, tot, turn).all_x;
+      there += scan<!LDS>((uint32_t)n, 0u, tot, turn).all_x;
     }
     from = first_tile == INT32_MAX ? 0 : (int64_t)first_tile * kTile;
   } else if (asked > 0) {
@@ -286,22 +297,13 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
     count();
     there = in_tile;
     at = 0;
-    // four tiles a round (64K pages: 2 us, and 1.5 a tile where they come one by one); a wavefront's 1024 of each fit 16 bits
+    // four tiles a round (144K pages: 18.8 us, and 21.5 where they come one by one); a tile's 16384 fit 16 bits
     for (int64_t base = kTile; base < a.n_pages && there < asked; base += 4 * kTile) {
       uint32_t n[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) n[i] = (uint32_t)__builtin_popcount(free_mask(a, base + i * kTile, w, lane));
-      const Sums s = scan(n[0] | n[1] << 16, n[2] | n[3] << 16, tot, turn);
-      (void)s;
-      uint32_t in[4] = {0, 0, 0, 0};
-      const uint2* const of = tot.of[turn ^ 1];
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        in[0] += of[i].x & 0xffffu;
-        in[1] += of[i].x >> 16;
-        in[2] += of[i].y & 0xffffu;
-        in[3] += of[i].y >> 16;
-      }
+      const Sums s = scan<!LDS>(n[0] | n[1] << 16, n[2] | n[3] << 16, tot, turn);
+      const uint32_t in[4] = {s.all_x & 0xffffu, s.all_x >> 16, s.all_y & 0xffffu, s.all_y >> 16};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (there == 0) from = base + i * kTile;
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void advance_kernel(const Args a) {
       // those that are refused pages or rows are the last ones that ask for any: the others' pages are the first ones
       if (n > 0 && need > 0) atomicMax(&most, rank[b] + need);
     }
-    const Sums s = scan((uint32_t)n, 0u, tot, turn);
+    const Sums s = scan<!LDS>((uint32_t)n, 0u, tot, turn);
     if (b < a.B) {
       start[b] = (int32_t)(rows + s.x);
       a.start[b] = (int32_t)(rows + s.x);

@@ -216,6 +216,16 @@ def test_rows(T):
             t.step(np.maximum(t.kv_len - 2, 0), n, twice=True)
 
 
+def test_rows_that_pass_32_bits():
+    """1023 sequences ask for 1023 * 4198405 = 2^32 + 1019 rows: the last one's row is not the 1020th."""
+    B, page, n = 1024, 1024, 4198405
+    t = Tables(B, page, 2 * B, 10000, n, n + 1)
+    t.refs[:B], t.table[:, 0], t.kv_len[:] = 1, np.arange(B), 1
+    t.put()
+    w = t.step(None, [n] * (B - 1) + [1])
+    assert (w["status"][:-1] == X.PAGES).all() and w["status"][-1] == X.ROWS and w["start"][-1] == 0
+
+
 def test_captured_and_replayed():
     """A graph follows keep, n_new and the tables; eager steps between its replays."""
     rng = np.random.default_rng(3)
