@@ -572,7 +572,8 @@ typedef struct lrqk_rope {
  *                     than `low` times are stretched
  *   LRQK_ROPE_RAMP    the same with s = 1 - (j - j0) / max(j1 - j0, 0.001) within [0, 1], linear in j from the pair that
  *                     turns `high` times to the one that turns `low` times: j(n) = rot ln(l_orig / (2 pi n)) / (2 ln base),
- *                     j0 = max(floor(j(high)), 0), j1 = min(ceil(j(low)), rot/2 - 1)
+ *                     j0 = max(floor(j(high)), 0), j1 = min(ceil(j(low)), rot - 1).  The pairs end at rot/2 - 1: if the last one
+ *                     turns more than `low` times, j1 lies behind it and no pair is stretched fully
  *   base      > 1;  factor > 0 (not looked at by PLAIN);  0 < low < high and l_orig >= 1 (BANDS and RAMP)
  *   turns      host, [rot/2]  written
  *   amplitude  host, may be NULL: written with 0.1 ln(factor) + 1 for RAMP (factor >= 1), 1 otherwise

@@ -320,7 +320,7 @@ LRQK_API int lrqk_rope_turns(int32_t rot, int32_t scaling, double base, double f
   if (scaling == LRQK_ROPE_RAMP) {
     auto index = [&](real n) { return rot * logl(l_orig / (two_pi * n)) / (2 * logl((real)base)); };
     j0 = std::fmax(floorl(index(high)), (real)0);
-    j1 = std::fmin(ceill(index(low)), (real)(rot / 2 - 1));
+    j1 = std::fmin(ceill(index(low)), (real)(rot - 1));  // (may lie behind the last pair, rot / 2 - 1: the pairs have a part of the ramp then)
   }
   for (int j = 0; j < rot / 2; ++j) {
     real f = powl(b, (real)(-2 * j) / rot);
