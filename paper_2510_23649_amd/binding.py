@@ -404,7 +404,9 @@ def lrqk_pages_workspace_bytes(shape: PagesShape) -> int:
     return load_library().lrqk_pages_workspace_bytes(C.byref(shape))
 
 
-_PAGE_TYPES = {torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2}
+# rows of 4 bits: uint8, and torch's own type where this torch has one
+_FOUR = tuple(t for t in (torch.uint8, getattr(torch, "float4_e2m1fn_x2", None)) if t is not None)
+_PAGE_TYPES = {torch.bfloat16, torch.float32, torch.uint8, torch.int8, torch.float8_e4m3fn, *_FOUR}
 
 
 def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pages:
@@ -423,7 +425,7 @@ def make_pages(*, K, V, table, start, kv_len, K_scale=None, V_scale=None) -> Pag
 
 
 _PAGE_ROWS = {LRQK_PAGE_BF16: (torch.bfloat16,), LRQK_PAGE_F32: (torch.float32,),
-              LRQK_PAGE_E2M1: (torch.uint8, torch.float4_e2m1fn_x2)}
+              LRQK_PAGE_E2M1: _FOUR}
 # what of a shape says how much its pages hold: B, Hkv and d, page to max_pages, page_dtype
 _HELD = [slice(getattr(PagesShape, a).offset, getattr(PagesShape, b).offset + 4)
          for a, b in (("B", "B"), ("Hkv", "d"), ("page", "max_pages"), ("page_dtype", "page_dtype"))]
