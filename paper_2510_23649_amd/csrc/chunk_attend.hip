@@ -718,6 +718,7 @@ __device__ __forceinline__ void put(const Args& a, const Problem& p, int kvh, in
 template <bool BF16, int PAGE>
 __device__ void add_left_out(const Args& a, const Problem& p, int kvh, int rows, int piece, int from, int to,
                              const float* sums, int states, int rows_held) {
+#pragma clang fp contract(off)  // (a code times its scale is the infinity that is added: fused with the sum it would be a number of any size)
   __syncthreads();  // what this workgroup has written is read below
   const int d = threadIdx.x % kD;
   for (int r = threadIdx.x / kD; r < rows; r += kThreads / kD) {
