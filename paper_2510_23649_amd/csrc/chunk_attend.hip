@@ -1256,6 +1256,51 @@ __device__ __forceinline__ uint4 cleared_chunk(uint4 x) {
   return make_uint4(clear<true>(x.x), clear<true>(x.y), clear<true>(x.z), clear<true>(x.w));
 }
 constexpr uint32_t kOddScale = 253;  // scale byte of e2m1 from which an element can be an infinity, or NaN
+enum { kPlus = 1, kMinus = 2, kNan = 4 };
+// What is not finite in the lane's 32 elements of each of the four tiles' rows, those that are there: `which`, by element.  A branch
+// that few blocks take.  256 tokens of 4 heads at 8K: 32 us without such elements, 44 with one block of them in every unit's way, 228 where V
+// holds nothing else (1962 with one block while a unit looked for it again at its end, position by position).
+__device__ __forceinline__ void note_odd(const uint4 (&v)[4], const uint32_t (&vs)[4], const uint32_t (&there)[4], int lane,
+                                         uint32_t* which, int& any) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (vs[i] < kOddScale || !((there[i] >> (lane & 15)) & 1)) continue;
+    const float f = scale_bits(vs[i]);
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t code = j == 0 ? v[i].x : j == 1 ? v[i].y : j == 2 ? v[i].z : v[i].w;
+      const uint4 y = decode8_bf16<LRQK_PAGE_E2M1>(code, f);
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t pair = e < 2 ? y.x : e < 4 ? y.y : e < 6 ? y.z : y.w, x = (e & 1 ? pair >> 16 : pair) & 0xffffu;
+        if ((x & 0x7f80u) != 0x7f80u) continue;
+        const uint32_t bit = x & 0x7fu ? kNan : x & 0x8000u ? kMinus : kPlus;
+        uint32_t* const to = which + 32 * (lane >> 4) + 8 * j + e;
+        if (!(*to & bit)) atomicOr(to, bit);  // (so that a context full of them does not wait for its atomics)
+        any = 1;
+      }
+    }
+  }
+}
+// Those given to all rows of the unit that have a weight.
+__device__ __forceinline__ void add_everywhere(const Args& a, const Problem& p, int kvh, int rows, uint32_t* which, const float* sums,
+                                               int rows_held) {
+  const int d = threadIdx.x % kD;
+  const uint32_t bits = which[d];
+  const float x = bits == kPlus ? INFINITY : bits == kMinus ? -INFINITY : __uint_as_float(0x7fc00000u);
+  for (int r = threadIdx.x / kD; bits && r < rows; r += kThreads / kD) {
+    bool any = a.partials != nullptr;  // (the join's to say)
+    for (int v = 0; v < kWaves; ++v) any |= sums[v * rows_held + r] != 0.0f;
+    if (!any) continue;
+    const int row = p.r0 + r;
+    const int64_t at = (int64_t)(p.s.first + row / a.G) * (a.m.Hkv * a.G) + kvh * a.G + row % a.G;
+    float* const to = a.partials ? a.partials + (at * a.pieces + p.piece) * kPartial + 4 + d : static_cast<float*>(a.out) + at * kD + d;
+    *to += x;  // (after add_left_out, whose thread has the same elements)
+  }
+  __syncthreads();
+  if (threadIdx.x < kD) which[threadIdx.x] = 0;
+  __syncthreads();
+}
 // Where LDS holds chunk c of a row of V: eight rows' same chunk (as they are stored) lies in eight places mod 8, eight rows' two
 // chunks (as they are read) in sixteen.
 __device__ __forceinline__ int few_chunk(int row, int c) {
@@ -1285,10 +1330,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
   const int kvh = blockIdx.x % a.m.Hkv;
   const uint4* const K = static_cast<const uint4*>(a.K);
   const uint4* const V = static_cast<const uint4*>(a.V);
-  __shared__ int odd_from[2];  // fp32: first block that something was left out of, in this unit and the next
+  // fp32: what was left out of blocks that every row of the unit sees, by element; whether that is anything, in this unit and the next
+  __shared__ uint32_t everywhere[BF16 ? 1 : kD];
+  __shared__ int any_everywhere[2];
   int turn = 0;
-  if (!BF16) {
-    if (threadIdx.x < 2) odd_from[threadIdx.x] = INT32_MAX;
+  if constexpr (!BF16) {
+    if (threadIdx.x < kD) everywhere[threadIdx.x] = 0;
+    if (threadIdx.x < 2) any_everywhere[threadIdx.x] = 0;
     __syncthreads();
   }
   Problem p;
@@ -1350,7 +1398,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
       bool far = false;
       for (int p0 = mine; p0 < end; p0 += kStep) {
         const bool part = p0 + BN > least, more = p0 + kStep < end;
-        // fp32: what is not finite is left out wherever it is, since it would meet weights' terms that are 0
+        // fp32: what is not finite is left out wherever it is, since it would meet weights' terms that are 0.  In blocks that every row of
+        // the unit sees it is noted here, element by element, and not looked for again
         const bool leave_out = part || (!BF16 && __any(max(max(vs[0], vs[1]), max(vs[2], vs[3])) >= kOddScale));
         const bool whole = !part && (there[0] & there[1] & there[2] & there[3]) == 0xffffu;
         bool left = false;
@@ -1375,8 +1424,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
             *reinterpret_cast<uint4*>(vt + few_chunk(16 * i + (lane & 15), 4 * (lane >> 4) + j)) = y;
           }
         }
-        cleared |= left;
-        if (!BF16 && left) atomicMin(&odd_from[turn], p0);
+        if (BF16 || part) {
+          cleared |= left;
+        } else if (__builtin_expect(leave_out, 0)) {
+          if constexpr (!BF16) note_odd(v, vs, now, lane, everywhere, any_everywhere[turn]);
+        }
         if (more) {
           find(p0 + kStep);
           fetch(V, a.V_scale, v, vs);
@@ -1477,9 +1529,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(const Args a) {
       const int64_t at = (int64_t)(p.s.first + row / a.G) * (a.m.Hkv * a.G) + kvh * a.G + row % a.G;
       a.partials[at * a.pieces * kPartial + 2] = __int_as_float(max(1, (most + p.step - 1) / p.step));
     }
-    if (!BF16 && threadIdx.x == 0) odd_from[turn ^ 1] = INT32_MAX;  // (nobody looks at that one before the next unit)
+    if (!BF16 && threadIdx.x == 0) any_everywhere[turn ^ 1] = 0;  // (nobody looks at that one before the next unit)
     if (__syncthreads_or(cleared))
-      add_left_out<BF16, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, BF16 ? max(from, least - least % BN) : odd_from[turn], end, ws, kWaves, M);
+      add_left_out<BF16, LRQK_PAGE_E2M1>(a, p, kvh, rows, p.piece, max(from, least - least % BN), end, ws, kWaves, M);
+    if constexpr (!BF16) {
+      if (any_everywhere[turn]) add_everywhere(a, p, kvh, rows, everywhere, ws, M);
+    }
     turn ^= 1;
   }
 }
