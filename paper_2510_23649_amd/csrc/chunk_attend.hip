@@ -1830,16 +1830,19 @@ hipError_t launch(const lrqk_pages_shape& s, const Cut& c, const Args& a, hipStr
   const int most = std::max(1, (c.few && c.want == 0 ? 1 << 20 : kFewGrid) / s.Hkv);
   const dim3 grid((unsigned)(s.Hkv * (c.rows == 128 ? c.units : std::min(c.units, most))));
   hipError_t e = hipSuccess;
+  constexpr bool k4 = PAGE == LRQK_PAGE_E2M1;  // (those go the few way wherever others go thin or in pairs, and in fp32 always: cut)
   if (s.page < 16) e = launch_thin<BF16, PAGE, true>(grid, a, st);
   else if (c.few) {
-    if constexpr (PAGE == LRQK_PAGE_E2M1) {
+    if constexpr (k4) {
       if (c.rows == 16) hipLaunchKernelGGL((attend_few_kernel<1, BF16>), grid, dim3(kThreads), 0, st, a);
       else if constexpr (BF16) hipLaunchKernelGGL((attend_few_kernel<2, BF16>), grid, dim3(kThreads), 0, st, a);
     }
-  } else if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
-  else if (c.rows == 64) {
-    if constexpr (BF16) hipLaunchKernelGGL((attend_pair_kernel<PAGE>), grid, dim3(kThreads), 0, st, a);
-  } else hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
+  } else if (c.rows == 128) {
+    if constexpr (BF16 || !k4) hipLaunchKernelGGL((attend_tile_kernel<BF16, PAGE>), grid, dim3(kThreads), 0, st, a);
+  } else if constexpr (!k4) {
+    if (c.rows == 32) e = launch_thin<BF16, PAGE, false>(grid, a, st);
+    else if constexpr (BF16) hipLaunchKernelGGL((attend_pair_kernel<PAGE>), grid, dim3(kThreads), 0, st, a);
+  }
   if (e != hipSuccess) return e;
   if (a.partials) {
     const int64_t rows = (int64_t)s.T * s.Hq;
