@@ -642,6 +642,9 @@ int lrqk_pages_rotate_append(const lrqk_pages_shape* shape, const lrqk_pages* pa
  *   status   per sequence: LRQK_ADVANCE_*
  *   seq, pos, slot   per packed row: its sequence, its position, and the row of the pool (page * table[b][pos / page] +
  *            pos mod page); -1 for rows that belong to no sequence.  Each may be NULL
+ * A sequence whose next row lies on a shared page (LRQK_ADVANCE_SHARED) goes on once the caller has given it a copy: a free page new for
+ * the page old of its table, K, V and their scales of old copied to new in every layer's pool (whole pages, plain device copies), refs[old] one less,
+ * refs[new] = 1, the table's entry new.  Prefixes that are whole pages need none.
  */
 typedef struct lrqk_pages_tables {
   int32_t* refs;    /* [n_pages]      read and updated */
