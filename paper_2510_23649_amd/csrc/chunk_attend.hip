@@ -1314,9 +1314,11 @@ __device__ __forceinline__ int few_chunk(int row, int c) {
 // One set: bound by memory where there is enough of it: one token of 16 sequences of 8K to 128K, 1.10 GB, 202 us and 5 for the
 // join, 5.4 TB/s (as thin workgroups 265); vector instructions are busy 37 % of the cycles, matrix cores 13 %, no LDS bank
 // conflict.  Blocks two ahead changed nothing; three wavefronts a SIMD do not get the registers without spilling (340 us).  One token at
-// 4K: 6.7 us and 2.6, a chain of loads that wait for each other.  Two sets: bound by the latency of what a block does one after
+// 4K: 7.4 us and 3.4, a chain of loads that wait for each other.  Two sets: bound by the latency of what a block does one after
 // the other, two wavefronts a SIMD covering it; 28 rows of 8 sequences of 32K, 285 MB, 76 to 82 us (thin 128); 1 to 5
-// tokens of 8 sequences of 7K to 64K, 7 heads a group, 99 MB, 40 us and 4 (pairs 48 and 6).  Three sets spill 200 bytes.
+// tokens of 8 sequences of 7K to 64K, 7 heads a group, 99 MB, 40 us and 4 (pairs 48 and 6).  Three sets spill 200 bytes.  Both
+// sets are worked on for a call with n_max for more than 16 rows, also if a sequence brings one token: 265 us for 16 sequences of up to 128K
+// (208 with n_max for 16 rows), 51 for 64 of up to 4K (44), 12.2 for one of 4K (11.3).
 // fp32, one set, bound by the products and the vector instructions about them: with the joins, one token of 16 sequences of up to 128K
 // 293 us (on the fp32 matrix cores, 32 rows a tile, 2486), the drafts 58 (399), 1001 tokens at 5003 and 744 at 1315 283 (676), 2048 tokens
 // at 32K 3.3 ms, 322 TFLOP/s (8.3).
@@ -1666,7 +1668,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const Args a, int
 // The same for attend_few_kernel's states: the number of a row's pieces stands with its first one, so that a row asks for
 // everything at once, its first states before it knows how many there are, and nothing depends on the number of sequences (a
 // token of 256 sequences, 8192 rows: 101 us in attend_join_kernel, where every row looks through their lengths; the whole call 281 us with
-// that and 198 with this).  2.5 us for a token at 4K, 16 pieces.  W wavefronts a row:
+// that and 198 with this).  2.4 to 3.4 us for a token at 4K, 16 pieces.  W wavefronts a row:
 // all of them weigh all pieces, each adds up every W-th.
 template <bool BF16, int W>
 __global__ __launch_bounds__(kThreads) void attend_join_few_kernel(const Args a, int64_t n_rows) {
@@ -1745,7 +1747,8 @@ constexpr int kFewGrid = 512;  // workgroups of a thin or pair launch, at most
 // 128 and 82, 32 rows 76 and 52, 35 rows in pairs 73 and 75, 1 to 35 rows 56 and 48, 63 rows 34.6 and 34.1; in fp32 all calls (see
 // attend_few_kernel).  Else at most 32 rows a
 // sequence and KV head go the thin way, and all calls with pages of less than 16 positions, whose rows have a place each (2048 tokens at 32K, bf16: 2360 us, and 1050 with pages of 16 and more; 12 tokens 38 and
-// 35; one token at 128K 114 and 106); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
+// 35; one token at 128K 114 and 106; pages of 4 bits with 8 and with 16 positions: one token of 16 sequences of 32K 206 and 121, five of 8
+// of 16K, 7 heads a group, 97 and 50, 1024 at 8K 258 and 185, in fp32 818 and 152, 215 and 67, 1397 and 431); up to 64 in pairs (bf16; in fp32 a pair's registers do not go twice on a compute unit);
 // more in tiles.
 struct Cut {
   int rows;  // 16: few, 32: few or thin, 64: pair, 128: tile

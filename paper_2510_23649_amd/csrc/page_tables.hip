@@ -20,8 +20,9 @@ constexpr int kTile = kThreads * 16;  // pages looked at together: a wavefront t
 constexpr int kRowsHere = 6144;
 constexpr int kSmall = 2;  // pages of a sequence that its own thread gives back or takes
 // Pages that the one workgroup looks through itself, as far as it has to: 3.6 us for 64K of them.  Two launches before it that give pages
-// back and count take 5.4, however many there are.  256 sequences of one token, 64K to 144K pages: 9.8 us where free ones lie in front and
-// 15.1 to 18.8 where only the last ones are free, 15.2 to 15.6 with counts; 1M pages at their end 15.4 with counts and 113 without.
+// back and count take 5, however many there are.  256 sequences that ask for a page each, in us a call without / with counts: a tenth
+// of the pool free, all over (requests come and go) 10.6 / 15.7 at 20K to 144K pages; the last tenth free (a pool that is filled from the front)
+// 14.8 / 15.3 at 20K, 15.2 / 15.6 at 64K and 90K, 18.9 / 15.5 at 144K; 1M pages at their end 113 / 15.4.
 constexpr int kPagesHere = 9 * kTile;
 
 struct Args {
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const Args a) {
   if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)s.all_x;
 }
 
-// 6.7 us for one sequence of one token, 9.7 for 256 (3.8 for a launch that finds nothing to do): a round trip to memory each for the
+// 6.5 us for one sequence of one token and a page, 9.6 for 256 (3.6 for a launch that finds nothing to do): a round trip to memory each for the
 // lengths, the entries given back, their references, the pool's, the table and its entries for the slots, and ten barriers.  What
 // most of them share lies in LDS, so that they wait for no store or load; with barriers that do, and all sixteen totals of a scan read by
 // every thread (128 registers and 19 spilled; now 86), 8.5 and 11.6.

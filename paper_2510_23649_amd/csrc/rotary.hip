@@ -6,7 +6,7 @@
 // (or some of its heads): lane j makes the cosine and sine of pair j once, LDS deals them out, and sixteen lanes turn a row of 128
 // elements, eight each, four rows at a time.
 // Bound by memory: 32768 tokens of 32 + 8 heads, bf16, 671 MB, 122 us (5.5 TB/s), 16384 in fp32 131 us; for few tokens by the latency of
-// a launch, the positions and the angles: 1 to 64 tokens 2.6 to 2.7 us.
+// a launch, the positions and the angles: 1 token 2.7 us, 16 and 64 tokens 3.6 by a kernel trace, 3.0 to 3.3 a call in a captured run of twenty.
 #include "pages.h"
 
 #include <cmath>
@@ -208,7 +208,7 @@ struct NewArgs {
 };
 
 // As r1; k and v go on into their pages.  Bound by memory: 15939 tokens of 4 prompts into pages of 4 bits, 343 MB, 66 us (5.2 TB/s); one
-// token of 16 sequences 2.9 us with positions and slots at hand, 3.9 from the tables (start, then length, then table).
+// token of 16 sequences 3.7 us with positions and slots at hand, 4.6 from the tables (start, then length, then table).
 template <bool BF16, int PAGE>
 __global__ __launch_bounds__(kThreads) void rotate_append_kernel(const NewArgs s) {
   constexpr int kRow = kD * (BF16 ? 2 : 4);
@@ -272,8 +272,8 @@ __global__ __launch_bounds__(kThreads) void rotate_append_kernel(const NewArgs s
   rows(false, s.v + t * s.v_stride, s.V, s.V_scale, max(from, v0) - v0, min(to, quads) - v0);
 }
 
-// Wavefronts a token: two for each of the chip's 1024 SIMDs, a quad of rows each at least.  In us with 1 / 512 / 2048 / 8192 of them:
-// 64 tokens 5.4 / 2.9 / 2.7 / 2.7, 256 5.6 / 4.2 / 3.5 / 3.6, 1024 6.7 / 6.7 / 5.7 / 7.2, 4096 14.7 / 14.8 / 14.7 / 14.4.
+// Wavefronts a token: two for each of the chip's 1024 SIMDs, a quad of rows each at least.  In us a call of a captured run of twenty
+// with 1 / 512 / 2048 / 8192 of them, bf16: 64 tokens 5.6 / 3.2 / 3.0 / 3.0, 256 5.9 / 4.5 / 3.8 / 3.8, 1024 6.9 / 6.9 / 5.9 / 7.4, 4096 15.0 / 14.9 / 15.0 / 14.5.
 int parts_of(int T, int quads) {
   const int want = (2048 + T - 1) / T;
   return want < 1 ? 1 : want > quads ? quads : want;
