@@ -549,7 +549,7 @@ int lrqk_chunk_attend(const lrqk_pages_shape* shape, const lrqk_pages* pages, co
  *   y_u = amplitude (x_u cos a - x_v sin a),   y_v = amplitude (x_v cos a + x_u sin a)
  *   LRQK_ROPE_HALVES  u = j, v = j + rot/2;     LRQK_ROPE_PAIRS  u = 2 j, v = 2 j + 1
  * The fraction is exact for every position (an integer product mod 2^64): far positions lose nothing.  Sums are
- * fp32; a result is off by at most 8 2^-24 amplitude (|x_u| + |x_v|), and the rounding to its type.
+ * fp32; a result is off by at most 8 2^-24 |amplitude| (|x_u| + |x_v|), and the rounding to its type.
  *   rot        even, 2 <= rot <= d
  *   back       0, or 1: by -a, the transposed map: what turns gradients back (and, up to amplitude^2, undoes it)
  *   amplitude  finite
