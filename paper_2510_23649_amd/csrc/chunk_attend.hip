@@ -322,12 +322,12 @@ struct Block {
       find_rows(a, b, kvh, f.p0, end, lane, at);
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        if constexpr (kLanes == kRow16) {  // (sums in 64 bits cost registers and 1 to 3 % of the time)
+        if constexpr (PAGE != LRQK_PAGE_E2M1) {  // (sums in 64 bits cost registers and 1 to 3 % of the time; for 4 bits sums in 32 cost 4 %)
           r.x[i] = static_cast<const Raw*>(base)[(size_t)(at[i] + c)];
           if constexpr (coded(PAGE)) r.scale[i] = scale[(size_t)((at[i] + c) / (kLanes / kScales))];
         } else {
           r.x[i] = static_cast<const Raw*>(base)[(size_t)at[i] * (kLanes / kRow16) + c];
-          if constexpr (coded(PAGE)) r.scale[i] = scale[(size_t)(at[i] / (kRow16 / kScales)) + c * kScales / kLanes];
+          r.scale[i] = scale[(size_t)(at[i] / (kRow16 / kScales)) + c * kScales / kLanes];
         }
       }
     } else {
