@@ -529,7 +529,8 @@ int lrqk_pages_read(const lrqk_pages_shape* shape, const lrqk_pages* pages, int3
  * over the positions that exist (their pages too), K and V of KV head h / G.  A token that sees no
  * position, or only scores of -infinity, gets zeros.  What a token does not see does not reach its
  * output, whatever its rows hold.  An infinite element of V under a weight of 0 (a score of -infinity, or one
- * that far below the others) makes NaN or that infinity.  Products of bf16 operands are exact, sums fp32; with bf16 q the
+ * that far below the others) makes NaN or that infinity.  Finite elements of V from 2^92 on may make infinities (a weight is up to 2^12
+ * before the sum of up to 2^24 of them divides it).  Products of bf16 operands are exact, sums fp32; with bf16 q the
  * weights are rounded to bf16 before they meet V and before they are summed.
  * (fp32 q over 4-bit pages of 16 positions and more: q and the weights are taken as three bf16 terms each that add up to
  * them exactly, but for terms below 2^-126.)
